@@ -484,6 +484,94 @@ int picasso_f2v_backward(picasso_ctx* ctx, void* stream, const float* d_gx, cons
                          const float* d_pi, int32_t T, const float* d_w, const int32_t* d_facets,
                          const int32_t* d_offsets, int32_t N, float* d_gy, float* d_gw, float* d_gpi);
 
+/* ---------------------------------------------------------------------------
+ * Layer norm, attention, gradient clipping: what the blocks of a mesh network
+ * need beside the convolutions, forward and backward.
+ *
+ * These calls only queue kernels on `stream` of the context's device: they wait for
+ * nothing, allocate nothing, keep nothing in the context (several may be under way
+ * at once, on one context too, from several threads, if each has a workspace of its own) and can be
+ * recorded into a graph.  The device that is current stays current.  A workspace is device memory of the caller's, 16-byte
+ * aligned, of the bytes that the operator's _workspace_bytes call names for the same sizes;
+ * its contents need not be kept between calls (two graphs may share one only if they
+ * never run at the same time); too small or NULL: PICASSO_ERR_WORKSPACE.
+ * Features are of one of the types below, all arithmetic is binary32 or more, a result is
+ * rounded once; parameters, their gradients and statistics are float32.  Sums are made in a
+ * fixed order, without atomics.  Outputs do not overlap inputs, unless said so; where that is seen the call is refused.
+ * ------------------------------------------------------------------------- */
+enum picasso_type {
+    PICASSO_F32 = 0,  /* binary32 */
+    PICASSO_BF16 = 1, /* bfloat16 */
+    PICASSO_F16 = 2   /* binary16 */
+};
+
+/* Layer norm over the rows of d_x [N,C]: y = gamma (x - mean) rstd + beta with the row's
+ * mean and rstd = 1 / sqrt(variance + eps) (the mean of the squared differences).
+ * d_gamma, d_beta [C] float32 (NULL: 1, 0).  d_y [N,C]; d_mean, d_rstd [N] (float32, may be
+ * NULL) are what the backward pass takes.  N >= 0, any C >= 1, finite eps >= 0; arrays aligned to a value. */
+int picasso_layer_norm_forward(picasso_ctx* ctx, void* stream, int type, const void* d_x, int32_t N, int32_t C,
+                               const float* d_gamma, const float* d_beta, float eps, void* d_y, float* d_mean,
+                               float* d_rstd);
+
+/* Its backward pass: d_gx [N,C] with respect to x, d_ggamma and d_gbeta [C] (float32) summed
+ * over the rows (0 for N = 0); each may be NULL, not all.  The workspace is for the sums (not needed without them). */
+size_t picasso_layer_norm_workspace_bytes(int type, int32_t N, int32_t C);
+int picasso_layer_norm_backward(picasso_ctx* ctx, void* stream, int type, const void* d_gy, const void* d_x, int32_t N,
+                                int32_t C, const float* d_gamma, const float* d_mean, const float* d_rstd, void* d_gx,
+                                float* d_ggamma, float* d_gbeta, void* d_workspace, size_t workspace_bytes);
+
+/* An array [T, H, D] of heads: element d of head h of row t is data[t * row_stride + h *
+ * head_stride + d] (strides in elements, both multiples of 16 bytes, data 16-byte aligned): whole arrays
+ * and parts of a projection's output alike. */
+typedef struct picasso_heads {
+    void* data;
+    int64_t row_stride, head_stride;
+} picasso_heads;
+
+/* Attention within packed sequences, such as the meshes of a mini-batch (Sec. 3: "mini-batches
+ * of concatenated meshes").  Sequence b has the queries d_q_offsets[b] .. d_q_offsets[b+1] of q
+ * [Tq,Hq,D] and the keys d_k_offsets[b] .. d_k_offsets[b+1] of k and v [Tk,Hkv,D] (the same vertices,
+ * another level's, or, for a readout, many keys for one query); any lengths, 0 included.
+ * Offsets are ascending int32 device arrays [B+1]; ones outside [0, T] are clipped, ones that
+ * descend give unspecified results within the arrays.  Head h of q goes with head h / (Hq / Hkv) of k and v.
+ *   s_ij = scale <q_i, k_j>,  p_ij = exp(s_ij) / sum_j exp(s_ij),  out_i = sum_j p_ij v_j,  lse_i = log sum_j exp(s_ij)
+ * over the keys j of the sequence, numbered from its first; causal: over those with j <= i + (lk - lq), so that the
+ * last query sees all.  A query that sees no key gets out = 0, lse = -inf.  out [Tq,Hq,D], d_lse [Hq,Tq] float32 (may be NULL).
+ * Rows of no sequence (in front of the first, behind the last) are left as they were, or, with clear_outside, get what
+ * a query without keys gets.  A causal call's non-finite keys and values may reach queries in front of them; those of
+ * another sequence or of rows of none never do.  Hq a multiple of Hkv (at most 65535), D a multiple of 8 up to 128,
+ * Tq * Hq / Hkv and Tk up to 2^30, B up to 2^24, scale finite and positive. */
+size_t picasso_attention_workspace_bytes(int type, int32_t B, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv, int32_t D,
+                                         int backward);
+int picasso_attention_forward(picasso_ctx* ctx, void* stream, int type, const picasso_heads* q, const picasso_heads* k,
+                              const picasso_heads* v, const int32_t* d_q_offsets, const int32_t* d_k_offsets, int32_t B,
+                              int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv, int32_t D, int causal, float scale,
+                              int clear_outside, const picasso_heads* out, float* d_lse, void* d_workspace,
+                              size_t workspace_bytes);
+
+/* Its backward pass, from the forward pass's out and d_lse: gq, gk, gv (shaped as q, k, v; gk and gv summed over the
+ * heads of q that share them).  Rows of no sequence as above (cleared: 0). */
+int picasso_attention_backward(picasso_ctx* ctx, void* stream, int type, const picasso_heads* gout, const picasso_heads* q,
+                               const picasso_heads* k, const picasso_heads* v, const picasso_heads* out,
+                               const float* d_lse, const int32_t* d_q_offsets, const int32_t* d_k_offsets, int32_t B,
+                               int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv, int32_t D, int causal, float scale,
+                               int clear_outside, const picasso_heads* gq, const picasso_heads* gk,
+                               const picasso_heads* gv, void* d_workspace, size_t workspace_bytes);
+
+/* Norm of n tensors together, *d_norm = sqrt(sum of all values' squares) (float32; the sum is in
+ * 64 bits), and clipping by it: out = g * min(1, max_norm / (norm + 1e-6)).  h_grads, h_out
+ * (host arrays of device pointers), h_sizes (values), h_types (picasso_type) describe the tensors; they
+ * are read before the call returns.  h_out[k] may be h_grads[k]; no output overlaps another output or
+ * another tensor (a tensor listed twice is refused).  max_norm >= 0, may be infinite.  A norm that is NaN
+ * makes everything NaN, an infinite one makes finite gradients 0 and infinite ones NaN.
+ * d_norm may be NULL in picasso_clip_gradients.  n >= 0, sizes >= 0. */
+size_t picasso_gradients_workspace_bytes(int32_t n, const int64_t* h_sizes);
+int picasso_gradient_norm(picasso_ctx* ctx, void* stream, int32_t n, const void* const* h_grads, const int64_t* h_sizes,
+                          const int32_t* h_types, float* d_norm, void* d_workspace, size_t workspace_bytes);
+int picasso_clip_gradients(picasso_ctx* ctx, void* stream, int32_t n, const void* const* h_grads, const int64_t* h_sizes,
+                           const int32_t* h_types, double max_norm, void* const* h_out, float* d_norm, void* d_workspace,
+                           size_t workspace_bytes);
+
 #ifdef __cplusplus
 }
 #endif

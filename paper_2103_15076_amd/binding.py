@@ -64,9 +64,17 @@ EXPORTED_SYMBOLS = (
     "picasso_v2f_backward", "picasso_f2f_forward", "picasso_f2f_backward", "picasso_f2f_clear_unowned", "picasso_f2v_forward",
     "picasso_f2v_backward", "picasso_pool_forward",
     "picasso_pool_backward", "picasso_unpool_forward", "picasso_unpool_backward",
+    "picasso_layer_norm_forward", "picasso_layer_norm_workspace_bytes", "picasso_layer_norm_backward",
+    "picasso_attention_workspace_bytes", "picasso_attention_forward", "picasso_attention_backward",
+    "picasso_gradients_workspace_bytes", "picasso_gradient_norm", "picasso_clip_gradients",
 )
 
 PICASSO_POOL_AVG, PICASSO_POOL_MAX, PICASSO_POOL_WEIGHTED, PICASSO_POOL_SUM = 0, 1, 2, 3
+PICASSO_F32, PICASSO_BF16, PICASSO_F16 = 0, 1, 2
+
+
+class picasso_heads(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("row_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64)]
 
 
 class picasso_stats(ctypes.Structure):
@@ -179,6 +187,29 @@ def load_library():
     lib.picasso_unpool_backward.argtypes = [vp, vp, vp, i32, i32, vp, vp, i32, vp]
     lib.picasso_bucket_sort.restype = ctypes.c_int
     lib.picasso_bucket_sort.argtypes = [vp, vp, ctypes.c_int, vp, vp, i64, ctypes.c_int]
+    size, hp, f32 = ctypes.c_size_t, ctypes.POINTER(picasso_heads), ctypes.c_float
+    sizes = [i32, i32, i32, i32, i32, i32]  # B, Tq, Tk, Hq, Hkv, D
+    ptrs, i64s, i32s = ctypes.POINTER(vp), ctypes.POINTER(i64), ctypes.POINTER(i32)
+    lib.picasso_layer_norm_forward.restype = ctypes.c_int
+    lib.picasso_layer_norm_forward.argtypes = [vp, vp, ctypes.c_int, vp, i32, i32, vp, vp, f32, vp, vp, vp]
+    lib.picasso_layer_norm_workspace_bytes.restype = size
+    lib.picasso_layer_norm_workspace_bytes.argtypes = [ctypes.c_int, i32, i32]
+    lib.picasso_layer_norm_backward.restype = ctypes.c_int
+    lib.picasso_layer_norm_backward.argtypes = [vp, vp, ctypes.c_int, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, vp, size]
+    lib.picasso_attention_workspace_bytes.restype = size
+    lib.picasso_attention_workspace_bytes.argtypes = [ctypes.c_int] + sizes + [ctypes.c_int]
+    lib.picasso_attention_forward.restype = ctypes.c_int
+    lib.picasso_attention_forward.argtypes = ([vp, vp, ctypes.c_int, hp, hp, hp, vp, vp] + sizes +
+                                              [ctypes.c_int, f32, ctypes.c_int, hp, vp, vp, size])
+    lib.picasso_attention_backward.restype = ctypes.c_int
+    lib.picasso_attention_backward.argtypes = ([vp, vp, ctypes.c_int, hp, hp, hp, hp, hp, vp, vp, vp] + sizes +
+                                               [ctypes.c_int, f32, ctypes.c_int, hp, hp, hp, vp, size])
+    lib.picasso_gradients_workspace_bytes.restype = size
+    lib.picasso_gradients_workspace_bytes.argtypes = [i32, i64s]
+    lib.picasso_gradient_norm.restype = ctypes.c_int
+    lib.picasso_gradient_norm.argtypes = [vp, vp, i32, ptrs, i64s, i32s, vp, vp, size]
+    lib.picasso_clip_gradients.restype = ctypes.c_int
+    lib.picasso_clip_gradients.argtypes = [vp, vp, i32, ptrs, i64s, i32s, ctypes.c_double, ptrs, vp, vp, size]
     _lib = lib
     return lib
 
@@ -432,6 +463,38 @@ class Context:
     def picasso_f2v_backward(self, gx, y, pi, w, facets, offsets, want_gpi=True, stream=None):
         """Returns (gy[F,C], gw[T,C], gpi[F,T] or None)."""
         return self._n.f2v_backward(self._p, stream, gx, y, pi, w, facets, offsets, bool(want_gpi))
+
+    # ---- layer norm, attention, gradient clipping.  Tensors are float32, bfloat16 or float16 on the context's device; stream
+    # None: that device's current stream.  Outputs and workspaces come from torch's allocator, call by call; the calls wait for
+    # nothing and can be recorded into graphs.
+
+    def picasso_layer_norm_forward(self, x, gamma=None, beta=None, eps=1e-5, out=None, stream=None):
+        """Rows of x [N, C] normalised, times gamma plus beta (float32 [C]).  Returns (y[N,C], mean f32[N], rstd f32[N])."""
+        return self._n.layer_norm_forward(self._p, self.device, stream, x, gamma, beta, eps, out)
+
+    def picasso_layer_norm_backward(self, gy, x, gamma, mean, rstd, stream=None):
+        """Returns (gx[N,C], ggamma f32[C], gbeta f32[C])."""
+        return self._n.layer_norm_backward(self._p, self.device, stream, gy, x, gamma, mean, rstd)
+
+    def picasso_attention_forward(self, q, k, v, q_offsets, k_offsets=None, causal=False, scale=None, out=None, stream=None):
+        """Attention of q [Tq, Hq, D] over k, v [Tk, Hkv, D] within the sequences that the offsets (int32 [B+1], on the device;
+        k_offsets None: the queries') mark off.  scale None: 1 / sqrt(D).  Returns (out[Tq,Hq,D], lse f32[Hq,Tq]); rows of no
+        sequence are 0 and -inf, or, in an ``out`` of the caller's, left as they were (those of lse are unspecified then)."""
+        return self._n.attention_forward(self._p, self.device, stream, q, k, v, q_offsets, k_offsets, bool(causal), scale, out)
+
+    def picasso_attention_backward(self, gout, q, k, v, out, lse, q_offsets, k_offsets=None, causal=False, scale=None,
+                                   grads=(None, None, None), stream=None):
+        """Returns (gq, gk, gv), shaped as q, k, v, in ``grads`` if given (where rows of no sequence are left as they were)."""
+        return self._n.attention_backward(self._p, self.device, stream, gout, q, k, v, q_offsets, k_offsets, bool(causal), scale,
+                                          out, lse, *grads)
+
+    def picasso_gradient_norm(self, grads, stream=None):
+        """The norm of all tensors of a sequence together, f32[1] on the device."""
+        return self._n.gradient_norm(self._p, self.device, stream, grads)
+
+    def picasso_clip_gradients(self, grads, max_norm, out=None, stream=None):
+        """grads (a sequence of tensors) times min(1, max_norm / (norm + 1e-6)), in place or into ``out``.  Returns the norm."""
+        return self._n.clip_gradients(self._p, self.device, stream, grads, max_norm, out)
 
     def picasso_bucket_sort(self, keys, vals=None, key_bits=None, stream=None):
         """Same as picasso_radix_sort, by top-digit partition + per-bucket LDS sort (n <= 2^20)."""

@@ -1,0 +1,522 @@
+// features.hip -- entry points of the operators on rows of features that blocks of a network need beside the convolutions:
+// layer norm (layer_norm.h), attention among packed sequences (attention.h), the norm of a network's gradients and clipping
+// (gradients.h).  A translation unit of its own, beside picasso.hip.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+#include <stdio.h>
+
+#include <algorithm>
+#include <vector>
+
+#include "../../include/picasso.h"
+#include "attention.h"
+#include "context.h"
+#include "gradients.h"
+#include "layer_norm.h"
+
+#pragma clang fp contract(off)
+
+namespace {
+
+// The context's device is current while an operator queues its work, and the one before it afterwards.
+struct OnDevice {
+    int before = -1, now;
+    hipError_t e;
+    explicit OnDevice(int device) : now(device) {
+        e = hipGetDevice(&before);
+        if (e == hipSuccess && before != now) e = hipSetDevice(now);
+    }
+    ~OnDevice() {
+        if (before >= 0 && before != now) (void)hipSetDevice(before);
+    }
+};
+
+int failed(picasso_ctx* c, hipError_t e, const char* what) {
+    char text[200];
+    snprintf(text, sizeof text, "%s: %s", what, hipGetErrorString(e));
+    picasso_note_hip_error(c, text);
+    return PICASSO_ERR_HIP;
+}
+#define ON_DEVICE(c)                           \
+    OnDevice on_device(picasso_device_of(c));  \
+    if (on_device.e != hipSuccess) return failed(c, on_device.e, "selecting the context's device")
+#define LAUNCHED(c)                                                      \
+    do {                                                                 \
+        const hipError_t e__ = hipGetLastError();                        \
+        if (e__ != hipSuccess) return failed(c, e__, "a kernel's launch"); \
+    } while (0)
+
+bool known_type(int type) { return type == PICASSO_F32 || type == PICASSO_BF16 || type == PICASSO_F16; }
+size_t size_of(int type) { return type == PICASSO_F32 ? 4 : 2; }
+size_t up(size_t x) { return (x + 255) / 256 * 256; }
+bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+
+// Whether two ranges of memory have a byte in common.
+bool meet(const void* a, size_t na, const void* b, size_t nb) {
+    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
+    return a && b && na && nb && x < y + nb && y < x + na;
+}
+
+// CALL(T) for the features' type
+#define FOR_TYPE(type, CALL)                           \
+    do {                                               \
+        if ((type) == PICASSO_F32) { CALL(feat::f32); }        \
+        else if ((type) == PICASSO_BF16) { CALL(feat::bf16); } \
+        else { CALL(feat::f16); }                      \
+    } while (0)
+
+// ---- layer norm -------------------------------------------------------------------------------------
+
+// Lanes that share a row of C features, and packs a lane: as few lanes as hold it with a pack each, up to a wave; then up to
+// four packs a lane; then a workgroup's lanes.
+struct NormShape {
+    int lanes, packs;
+};
+NormShape norm_shape(int C, int per_pack) {
+    const int q = (C + per_pack - 1) / per_pack;
+    NormShape s{1, 1};
+    while (s.lanes < 64 && s.lanes < q) s.lanes *= 2;
+    if (q > 256) s.lanes = feat::BLOCK;
+    while (s.lanes * s.packs < q) s.packs *= 2;
+    return s;
+}
+constexpr int NORM_MAX_PACKS = 8;
+
+#define NORM_SHAPES(T, s, CALL)                                                                                      \
+    do {                                                                                                             \
+        switch ((s).lanes) {                                                                                         \
+            case 1: CALL(T, 1, 1); break;                                                                            \
+            case 2: CALL(T, 2, 1); break;                                                                            \
+            case 4: CALL(T, 4, 1); break;                                                                            \
+            case 8: CALL(T, 8, 1); break;                                                                            \
+            case 16: CALL(T, 16, 1); break;                                                                          \
+            case 32: CALL(T, 32, 1); break;                                                                          \
+            case 64:                                                                                                 \
+                if ((s).packs == 1) CALL(T, 64, 1);                                                                  \
+                else if ((s).packs == 2) CALL(T, 64, 2);                                                             \
+                else CALL(T, 64, 4);                                                                                 \
+                break;                                                                                               \
+            default:                                                                                                 \
+                if ((s).packs == 2) CALL(T, 256, 2);                                                                 \
+                else if ((s).packs == 4) CALL(T, 256, 4);                                                            \
+                else if constexpr (sizeof(T) == 4) CALL(T, 256, 8);                                                  \
+        }                                                                                                            \
+    } while (0)
+
+// Workgroups of the backward pass, each with `chunk` rows and a partial sum of every column: as many as the chip holds at work
+// (four a compute unit), fewer where each would have less than a few turns of rows.
+struct NormSplit {
+    long long chunk;
+    int groups;
+};
+NormSplit norm_split(long long N, int C, int type) {
+    const NormShape s = norm_shape(C, 16 / (int)size_of(type));
+    const long long turn = C > lnorm::MAX_C ? 64 : 2ll * std::max(1, feat::BLOCK / s.lanes);
+    long long groups = std::max(1ll, std::min(1024ll, (N + 2 * turn - 1) / (2 * turn)));
+    const long long chunk = std::max(1ll, ((N + groups - 1) / groups + turn - 1) / turn) * turn;
+    return NormSplit{chunk, (int)std::max(1ll, (N + chunk - 1) / chunk)};
+}
+
+template <typename T>
+void launch_norm_forward(hipStream_t s, const T* x, long long N, int C, const float* gamma, const float* beta, float eps, T* y,
+                         float* mean, float* rstd) {
+    if (C > lnorm::MAX_C) {
+        lnorm::forward_wide_kernel<T><<<(unsigned)N, feat::BLOCK, 0, s>>>(x, C, gamma, beta, eps, y, mean, rstd);
+        return;
+    }
+    const NormShape shape = norm_shape(C, feat::Chunk<T>::N);
+#define PICASSO_CALL(T, L, P)                                                                                  \
+    do {                                                                                                       \
+        const long long per = (long long)lnorm::rows_in_flight<L, P>() * lnorm::rows_per_block<L>();             \
+        lnorm::forward_kernel<T, L, P><<<(unsigned)((N + per - 1) / per), feat::BLOCK, 0, s>>>(x, N, C, gamma, beta, eps, y, mean, rstd); \
+    } while (0)
+    NORM_SHAPES(T, shape, PICASSO_CALL);
+#undef PICASSO_CALL
+}
+
+template <typename T>
+void launch_norm_backward(hipStream_t s, const T* gy, const T* x, long long N, int C, const float* gamma, const float* mean,
+                          const float* rstd, T* gx, float* partial, const NormSplit& sp) {
+    if (C > lnorm::MAX_C) {
+        if (gx && N) lnorm::backward_wide_kernel<T><<<(unsigned)N, feat::BLOCK, 0, s>>>(gy, x, C, gamma, mean, rstd, gx);
+        if (partial)
+            lnorm::columns_wide_kernel<T><<<dim3(sp.groups, (C + feat::BLOCK - 1) / feat::BLOCK), feat::BLOCK, 0, s>>>(
+                gy, x, N, C, mean, rstd, sp.chunk, partial);
+        return;
+    }
+    const NormShape shape = norm_shape(C, feat::Chunk<T>::N);
+#define PICASSO_CALL(T, L, P) \
+    lnorm::backward_kernel<T, L, P><<<sp.groups, feat::BLOCK, 0, s>>>(gy, x, N, C, gamma, mean, rstd, sp.chunk, gx, partial)
+    NORM_SHAPES(T, shape, PICASSO_CALL);
+#undef PICASSO_CALL
+}
+
+// ---- attention --------------------------------------------------------------------------------------
+
+struct Attention {  // sizes of a call
+    int type, B, Tq, Tk, Hq, Hkv, D;
+    int G() const { return Hq / Hkv; }
+    long long rows() const { return (long long)Tq * G(); }
+};
+bool valid(const Attention& a) {
+    return known_type(a.type) && a.B >= 1 && a.B <= (1 << 24) && a.Tq >= 0 && a.Tk >= 0 && a.Tk <= (1 << 30) && a.Hq >= 1 && a.Hkv >= 1 &&
+           a.Hq % a.Hkv == 0 && a.Hkv <= 65535 && a.D >= 8 && a.D <= 128 && a.D % 8 == 0 && a.rows() <= (1ll << 30);
+}
+
+// Into how many parts an axis of `length` on average is split, where there are `groups` workgroups without: so that the chip has
+// two a compute unit, parts of at least `least`.
+int splits_for(long long groups, long long length, int least) {
+    const long long wanted = (512 + groups - 1) / std::max(1ll, groups);
+    return (int)std::max(1ll, std::min({wanted, length / least, 64ll}));
+}
+
+struct ForwardPlan {
+    int row_waves, splits;
+};
+ForwardPlan forward_plan(const Attention& a) {
+    const long long groups128 = (a.rows() / 128 + a.B) * a.Hkv, keys = a.Tk / a.B;
+    ForwardPlan p;
+    // short sequences and single tokens: 32 rows a workgroup, and too few groups of 128 to fill the chip
+    p.row_waves = a.rows() <= 48ll * a.B || groups128 < 256 ? 1 : 4;
+    const long long groups = p.row_waves == 4 ? groups128 : (a.rows() / 32 + a.B) * a.Hkv;
+    p.splits = splits_for(groups, keys, 256);
+    return p;
+}
+struct BackwardPlan {
+    int key_splits, query_splits;
+};
+BackwardPlan backward_plan(const Attention& a) {
+    BackwardPlan p;
+    p.key_splits = splits_for(((long long)a.Tk / 128 + a.B) * a.Hkv, a.rows() / a.B, 128);
+    p.query_splits = splits_for((a.rows() / 128 + a.B) * a.Hkv, a.Tk / a.B, 128);
+    return p;
+}
+
+size_t attention_forward_bytes(const Attention& a) {
+    const ForwardPlan p = forward_plan(a);
+    if (p.splits == 1) return 0;
+    return up((size_t)p.splits * a.Tq * a.Hq * a.D * 4) + up((size_t)p.splits * a.Tq * a.Hq * 4);
+}
+size_t attention_backward_bytes(const Attention& a) {
+    const BackwardPlan p = backward_plan(a);
+    const size_t keys = p.key_splits == 1 ? 0 : 2 * up((size_t)p.key_splits * a.Tk * a.Hkv * a.D * 4);
+    const size_t queries = p.query_splits == 1 ? 0 : up((size_t)p.query_splits * a.Tq * a.Hq * a.D * 4);
+    return up((size_t)a.Tq * a.Hq * 4) + std::max(keys, queries);
+}
+
+// An array of heads as the kernels take it: 16-byte aligned rows and heads.
+bool valid_heads(const picasso_heads* h, const Attention& a, int rows, bool output) {
+    if (!h || (rows > 0 && !h->data)) return false;
+    const long long each = (long long)(16 / size_of(a.type)), least = output ? a.D : 0;
+    return aligned(h->data, 16) && h->row_stride >= least && h->head_stride >= least && h->row_stride % each == 0 && h->head_stride % each == 0 &&
+           h->row_stride <= (1ll << 40) && h->head_stride <= (1ll << 40);
+}
+size_t extent(const picasso_heads* h, const Attention& a, int rows, int heads) {
+    return rows ? (size_t)((rows - 1) * h->row_stride + (heads - 1) * h->head_stride + a.D) * size_of(a.type) : 0;
+}
+template <typename T>
+attn::Heads<T> heads(const picasso_heads* h) {
+    return attn::Heads<T>{(T*)h->data, (long long)h->row_stride, (long long)h->head_stride};
+}
+
+// CALL(T, DP): features padded to 32, 64 or 128
+#define FOR_WIDTH(T, D, CALL)                      \
+    do {                                           \
+        if ((D) <= 32) { CALL(T, 32); }            \
+        else if ((D) <= 64) { CALL(T, 64); }       \
+        else { CALL(T, 128); }                     \
+    } while (0)
+
+// (outputs whose rows and heads interleave, as the parts of one projection do, may share a range of memory: only inputs are held
+// apart from outputs, and only where an output is a whole range by itself)
+bool dense(const picasso_heads* h, const Attention& a, int heads) { return h->head_stride == a.D && h->row_stride == (int64_t)heads * a.D; }
+
+// ---- gradients --------------------------------------------------------------------------------------
+
+struct GradientsPlan {
+    long long launches, partials;  // partials of all launches
+};
+template <typename Each>
+bool gradient_tables(int n, const void* const* in, void* const* out, const int64_t* sizes, const int32_t* types, Each each) {
+    const int launches = std::max(1, (n + grads::TENSORS - 1) / grads::TENSORS);
+    const int most = std::max(256, grads::MAX_PARTIALS / launches);
+    for (int at = 0; at < n; at += grads::TENSORS) {
+        grads::Table t;
+        t.count = std::min(grads::TENSORS, n - at);
+        unsigned long long chunks = 0;
+        for (int k = 0; k < t.count; ++k) {
+            t.in[k] = in ? in[at + k] : nullptr;
+            t.out[k] = out ? out[at + k] : nullptr;
+            t.size_type[k] = (unsigned long long)sizes[at + k] << 2 | (unsigned)(types ? types[at + k] : 0);
+            t.first[k] = (unsigned)chunks;
+            chunks += ((unsigned long long)sizes[at + k] + grads::CHUNK_VALUES - 1) / grads::CHUNK_VALUES;
+            if (chunks > 0x7FFFFFFFull) return false;
+        }
+        t.first[t.count] = (unsigned)chunks;
+        if (chunks) each(t, (int)std::min<unsigned long long>(chunks, most));
+    }
+    return true;
+}
+
+bool valid_gradients(int n, const void* const* in, const int64_t* sizes, const int32_t* types) {
+    if (n < 0 || (n > 0 && (!in || !sizes || !types))) return false;
+    for (int k = 0; k < n; ++k)
+        if (sizes[k] < 0 || sizes[k] > (1ll << 44) || !known_type(types[k]) || (sizes[k] > 0 && !in[k]) || !aligned(in[k], size_of(types[k])))
+            return false;
+    return true;
+}
+
+// Partials of all tensors' squares in ws; how many.
+int queue_squares(hipStream_t s, int n, const void* const* in, const int64_t* sizes, const int32_t* types, double* ws) {
+    int partials = 0;
+    gradient_tables(n, in, nullptr, sizes, types, [&](const grads::Table& t, int groups) {
+        grads::squares_kernel<<<groups, feat::BLOCK, 0, s>>>(t, ws + partials);
+        partials += groups;
+    });
+    return partials;
+}
+
+}  // namespace
+
+extern "C" {
+
+int picasso_layer_norm_forward(picasso_ctx* c, void* stream, int type, const void* d_x, int32_t N, int32_t C, const float* d_gamma,
+                               const float* d_beta, float eps, void* d_y, float* d_mean, float* d_rstd) {
+    if (!c || !known_type(type) || N < 0 || C < 1 || !(eps >= 0.0f) || !std::isfinite(eps) || (N > 0 && (!d_x || !d_y)))
+        return PICASSO_ERR_INVALID_ARG;
+    const size_t bytes = (size_t)N * C * size_of(type);
+    if (!aligned(d_x, size_of(type)) || !aligned(d_y, size_of(type)) || meet(d_x, bytes, d_y, bytes)) return PICASSO_ERR_INVALID_ARG;
+    if (N == 0) return PICASSO_OK;
+    hipStream_t s = (hipStream_t)stream;
+    ON_DEVICE(c);
+#define PICASSO_CALL(T) launch_norm_forward<T>(s, (const T*)d_x, N, C, d_gamma, d_beta, eps, (T*)d_y, d_mean, d_rstd)
+    FOR_TYPE(type, PICASSO_CALL);
+#undef PICASSO_CALL
+    LAUNCHED(c);
+    return PICASSO_OK;
+}
+
+size_t picasso_layer_norm_workspace_bytes(int type, int32_t N, int32_t C) {
+    if (!known_type(type) || N < 0 || C < 1) return 0;
+    return (size_t)norm_split(N, C, type).groups * 2 * C * sizeof(float);
+}
+
+int picasso_layer_norm_backward(picasso_ctx* c, void* stream, int type, const void* d_gy, const void* d_x, int32_t N, int32_t C,
+                                const float* d_gamma, const float* d_mean, const float* d_rstd, void* d_gx, float* d_ggamma,
+                                float* d_gbeta, void* d_workspace, size_t workspace_bytes) {
+    if (!c || !known_type(type) || N < 0 || C < 1 || (N > 0 && (!d_gy || !d_x || !d_mean || !d_rstd)) || (!d_gx && !d_ggamma && !d_gbeta))
+        return PICASSO_ERR_INVALID_ARG;
+    const size_t bytes = (size_t)N * C * size_of(type);
+    if (!aligned(d_gy, size_of(type)) || !aligned(d_x, size_of(type)) || !aligned(d_gx, size_of(type)) || meet(d_x, bytes, d_gx, bytes) ||
+        meet(d_gy, bytes, d_gx, bytes))
+        return PICASSO_ERR_INVALID_ARG;
+    const bool sums = d_ggamma || d_gbeta;
+    if (sums && (!d_workspace || workspace_bytes < picasso_layer_norm_workspace_bytes(type, N, C))) return PICASSO_ERR_WORKSPACE;
+    if (N == 0 && !sums) return PICASSO_OK;
+    hipStream_t s = (hipStream_t)stream;
+    ON_DEVICE(c);
+    const NormSplit sp = norm_split(N, C, type);
+    float* partial = sums ? (float*)d_workspace : nullptr;
+#define PICASSO_CALL(T) \
+    launch_norm_backward<T>(s, (const T*)d_gy, (const T*)d_x, N, C, d_gamma, d_mean, d_rstd, (T*)d_gx, partial, sp)
+    FOR_TYPE(type, PICASSO_CALL);
+#undef PICASSO_CALL
+    if (sums)
+        lnorm::finish_kernel<<<(unsigned)((2ll * C + lnorm::FINISH_COLS - 1) / lnorm::FINISH_COLS), feat::BLOCK, 0, s>>>(partial, sp.groups, C, d_ggamma,
+                                                                                                             d_gbeta);
+    LAUNCHED(c);
+    return PICASSO_OK;
+}
+
+size_t picasso_attention_workspace_bytes(int type, int32_t B, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv, int32_t D, int backward) {
+    const Attention a{type, B, Tq, Tk, Hq, Hkv, D};
+    if (!valid(a)) return 0;
+    return backward ? attention_backward_bytes(a) : attention_forward_bytes(a);
+}
+
+int picasso_attention_forward(picasso_ctx* c, void* stream, int type, const picasso_heads* q, const picasso_heads* k, const picasso_heads* v,
+                              const int32_t* d_q_offsets, const int32_t* d_k_offsets, int32_t B, int32_t Tq, int32_t Tk, int32_t Hq,
+                              int32_t Hkv, int32_t D, int causal, float scale, int clear_outside, const picasso_heads* out, float* d_lse,
+                              void* d_workspace, size_t workspace_bytes) {
+    const Attention a{type, B, Tq, Tk, Hq, Hkv, D};
+    if (!c || !valid(a) || !valid_heads(q, a, Tq, false) || !valid_heads(k, a, Tk, false) || !valid_heads(v, a, Tk, false) ||
+        !valid_heads(out, a, Tq, true) || !d_q_offsets || !d_k_offsets || !(scale > 0.0f) || !std::isfinite(scale))
+        return PICASSO_ERR_INVALID_ARG;
+    if (dense(out, a, Hq)) {
+        const size_t n = extent(out, a, Tq, Hq);
+        if (meet(out->data, n, q->data, extent(q, a, Tq, Hq)) || meet(out->data, n, k->data, extent(k, a, Tk, Hkv)) ||
+            meet(out->data, n, v->data, extent(v, a, Tk, Hkv)))
+            return PICASSO_ERR_INVALID_ARG;
+    }
+    const ForwardPlan p = forward_plan(a);
+    const size_t need = attention_forward_bytes(a);
+    if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16))) return PICASSO_ERR_WORKSPACE;
+    if (Tq == 0) return PICASSO_OK;
+    hipStream_t s = (hipStream_t)stream;
+    ON_DEVICE(c);
+    const attn::Offsets off{d_q_offsets, d_k_offsets, B, Tq, Tk};
+    const attn::Group group = attn::heads_per_group(a.G());
+    float* part_out = p.splits > 1 ? (float*)d_workspace : nullptr;
+    float* part_lse = p.splits > 1 ? (float*)((char*)d_workspace + up((size_t)p.splits * Tq * Hq * D * 4)) : nullptr;
+    const float scale2 = scale * attn::LOG2E;
+#define PICASSO_FORWARD(T, DP, W)                                                                                          \
+    attn::forward_kernel<T, DP, W>                                                                                         \
+        <<<dim3((unsigned)attn::tile_numbers(Tq, a.G(), 32 * W, B), Hkv, p.splits), feat::BLOCK, 0, s>>>(                   \
+            heads<const T>(q), heads<const T>(k), heads<const T>(v), off, Hq, Hkv, group, D, causal, clear_outside, scale2, \
+            heads<T>(out), d_lse, part_out, part_lse)
+#define PICASSO_WIDTH(T, DP)                               \
+    if (p.row_waves == 4) PICASSO_FORWARD(T, DP, 4);       \
+    else PICASSO_FORWARD(T, DP, 1)
+#define PICASSO_CALL(T)                                                                                                       \
+    FOR_WIDTH(T, D, PICASSO_WIDTH);                                                                                           \
+    if (p.splits > 1)                                                                                                         \
+    attn::join_kernel<T><<<(unsigned)(((long long)Tq * Hq * (D / 4) + feat::BLOCK - 1) / feat::BLOCK), feat::BLOCK, 0, s>>>(   \
+        part_out, part_lse, p.splits, off, Hq, D, clear_outside, heads<T>(out), d_lse)
+    FOR_TYPE(type, PICASSO_CALL);
+#undef PICASSO_CALL
+#undef PICASSO_WIDTH
+#undef PICASSO_FORWARD
+    LAUNCHED(c);
+    return PICASSO_OK;
+}
+
+int picasso_attention_backward(picasso_ctx* c, void* stream, int type, const picasso_heads* gout, const picasso_heads* q,
+                               const picasso_heads* k, const picasso_heads* v, const picasso_heads* out, const float* d_lse,
+                               const int32_t* d_q_offsets, const int32_t* d_k_offsets, int32_t B, int32_t Tq, int32_t Tk, int32_t Hq,
+                               int32_t Hkv, int32_t D, int causal, float scale, int clear_outside, const picasso_heads* gq,
+                               const picasso_heads* gk, const picasso_heads* gv, void* d_workspace, size_t workspace_bytes) {
+    const Attention a{type, B, Tq, Tk, Hq, Hkv, D};
+    if (!c || !valid(a) || !valid_heads(gout, a, Tq, false) || !valid_heads(q, a, Tq, false) || !valid_heads(k, a, Tk, false) ||
+        !valid_heads(v, a, Tk, false) || !valid_heads(out, a, Tq, false) || !valid_heads(gq, a, Tq, true) || !valid_heads(gk, a, Tk, true) ||
+        !valid_heads(gv, a, Tk, true) || (Tq > 0 && !d_lse) || !d_q_offsets || !d_k_offsets || !(scale > 0.0f) || !std::isfinite(scale))
+        return PICASSO_ERR_INVALID_ARG;
+    const picasso_heads* const outputs[3] = {gq, gk, gv};
+    const picasso_heads* const inputs[5] = {gout, q, k, v, out};
+    for (int i = 0; i < 3; ++i) {
+        const int rows = i ? Tk : Tq, heads_ = i ? Hkv : Hq;
+        if (!dense(outputs[i], a, heads_)) continue;
+        for (int j = 0; j < 5; ++j) {
+            const bool keys = j == 2 || j == 3;
+            if (meet(outputs[i]->data, extent(outputs[i], a, rows, heads_), inputs[j]->data,
+                     extent(inputs[j], a, keys ? Tk : Tq, keys ? Hkv : Hq)))
+                return PICASSO_ERR_INVALID_ARG;
+        }
+    }
+    if (!d_workspace || workspace_bytes < attention_backward_bytes(a) || !aligned(d_workspace, 16)) return PICASSO_ERR_WORKSPACE;
+    if (Tq == 0 && Tk == 0) return PICASSO_OK;
+    hipStream_t s = (hipStream_t)stream;
+    ON_DEVICE(c);
+    const BackwardPlan p = backward_plan(a);
+    const attn::Offsets off{d_q_offsets, d_k_offsets, B, Tq, Tk};
+    const attn::Group group = attn::heads_per_group(a.G());
+    const attn::Scale sc{scale * attn::LOG2E, scale};
+    float* delta = (float*)d_workspace;
+    float* part = (float*)((char*)d_workspace + up((size_t)Tq * Hq * 4));
+    float* part_v = p.key_splits > 1 ? (float*)((char*)part + up((size_t)p.key_splits * Tk * Hkv * D * 4)) : nullptr;
+#define PICASSO_KEYS(T, DP)                                                                                                       \
+    attn::backward_keys_kernel<T, DP><<<dim3((unsigned)attn::tile_numbers(Tk, 1, 128, B), Hkv, p.key_splits), feat::BLOCK, 0, s>>>( \
+        heads<const T>(gout), heads<const T>(q), heads<const T>(k), heads<const T>(v), d_lse, delta, off, Hq, Hkv, group, D,        \
+        causal, clear_outside, sc, heads<T>(gk), heads<T>(gv), part, part_v)
+#define PICASSO_QUERIES(T, DP)                                                                                                      \
+    attn::backward_queries_kernel<T, DP>                                                                                            \
+        <<<dim3((unsigned)attn::tile_numbers(Tq, a.G(), 128, B), Hkv, p.query_splits), feat::BLOCK, 0, s>>>(                        \
+            heads<const T>(gout), heads<const T>(q), heads<const T>(k), heads<const T>(v), d_lse, delta, off, Hq, Hkv, group, D,      \
+            causal, clear_outside, sc, heads<T>(gq), part)
+#define PICASSO_SUM(T, splits, part, offsets, rows, H, to)                                                                         \
+    attn::sum_kernel<T><<<(unsigned)(((long long)(rows) * (H) * (D / 4) + feat::BLOCK - 1) / feat::BLOCK), feat::BLOCK, 0, s>>>(     \
+        part, splits, offsets, B, rows, H, D, clear_outside, heads<T>(to))
+#define PICASSO_CALL(T)                                                                                              \
+    if (Tq > 0)                                                                                                      \
+        attn::delta_kernel<T><<<(unsigned)(((long long)Tq * Hq * 16 + feat::BLOCK - 1) / feat::BLOCK), feat::BLOCK, 0, s>>>( \
+            heads<const T>(gout), heads<const T>(out), Tq, Hq, D, delta);                                            \
+    if (Tk > 0) {                                                                                                    \
+        FOR_WIDTH(T, D, PICASSO_KEYS);                                                                               \
+        if (p.key_splits > 1) {                                                                                      \
+            PICASSO_SUM(T, p.key_splits, part, d_k_offsets, Tk, Hkv, gk);                                            \
+            PICASSO_SUM(T, p.key_splits, part_v, d_k_offsets, Tk, Hkv, gv);                                          \
+        }                                                                                                            \
+    }                                                                                                                \
+    if (Tq > 0) {                                                                                                    \
+        FOR_WIDTH(T, D, PICASSO_QUERIES);                                                                            \
+        if (p.query_splits > 1) PICASSO_SUM(T, p.query_splits, part, d_q_offsets, Tq, Hq, gq);                       \
+    }
+    FOR_TYPE(type, PICASSO_CALL);
+#undef PICASSO_CALL
+#undef PICASSO_SUM
+#undef PICASSO_QUERIES
+#undef PICASSO_KEYS
+    LAUNCHED(c);
+    return PICASSO_OK;
+}
+
+size_t picasso_gradients_workspace_bytes(int32_t n, const int64_t* h_sizes) {
+    if (n < 0 || (n > 0 && !h_sizes)) return 0;
+    for (int k = 0; k < n; ++k)
+        if (h_sizes[k] < 0 || h_sizes[k] > (1ll << 44)) return 0;
+    size_t partials = 0;
+    gradient_tables(n, nullptr, nullptr, h_sizes, nullptr, [&](const grads::Table&, int groups) { partials += groups; });
+    return std::max<size_t>(partials, 1) * sizeof(double);
+}
+
+int picasso_gradient_norm(picasso_ctx* c, void* stream, int32_t n, const void* const* h_grads, const int64_t* h_sizes,
+                          const int32_t* h_types, float* d_norm, void* d_workspace, size_t workspace_bytes) {
+    if (!c || !valid_gradients(n, h_grads, h_sizes, h_types) || !d_norm) return PICASSO_ERR_INVALID_ARG;
+    if (!d_workspace || !aligned(d_workspace, 8) || workspace_bytes < picasso_gradients_workspace_bytes(n, h_sizes)) return PICASSO_ERR_WORKSPACE;
+    hipStream_t s = (hipStream_t)stream;
+    ON_DEVICE(c);
+    double* ws = (double*)d_workspace;
+    const int partials = queue_squares(s, n, h_grads, h_sizes, h_types, ws);
+    grads::norm_kernel<<<1, feat::BLOCK, 0, s>>>(ws, partials, d_norm);
+    LAUNCHED(c);
+    return PICASSO_OK;
+}
+
+int picasso_clip_gradients(picasso_ctx* c, void* stream, int32_t n, const void* const* h_grads, const int64_t* h_sizes,
+                           const int32_t* h_types, double max_norm, void* const* h_out, float* d_norm, void* d_workspace,
+                           size_t workspace_bytes) {
+    if (!c || !valid_gradients(n, h_grads, h_sizes, h_types) || !(max_norm >= 0.0) || (n > 0 && !h_out)) return PICASSO_ERR_INVALID_ARG;
+    for (int k = 0; k < n; ++k)
+        if ((h_sizes[k] > 0 && !h_out[k]) || !aligned(h_out[k], size_of(h_types[k]))) return PICASSO_ERR_INVALID_ARG;
+    if (!d_workspace || !aligned(d_workspace, 8) || workspace_bytes < picasso_gradients_workspace_bytes(n, h_sizes)) return PICASSO_ERR_WORKSPACE;
+    // an output may be its own gradient, and nothing else: a tensor that is listed twice would be scaled twice, or once and a half
+    {
+        struct Range {
+            uintptr_t from, to;
+            bool out;
+        };
+        std::vector<Range> r;
+        try {
+            r.reserve(2 * (size_t)n);
+            for (int k = 0; k < n; ++k) {
+                const uintptr_t bytes = (uintptr_t)h_sizes[k] * size_of(h_types[k]);
+                if (!bytes) continue;
+                r.push_back(Range{(uintptr_t)h_out[k], (uintptr_t)h_out[k] + bytes, true});
+                if (h_out[k] != h_grads[k]) r.push_back(Range{(uintptr_t)h_grads[k], (uintptr_t)h_grads[k] + bytes, false});
+            }
+        } catch (...) {
+            return PICASSO_ERR_WORKSPACE;
+        }
+        std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+        uintptr_t end_out = 0, end_any = 0;  // of those that start before
+        for (const Range& x : r) {
+            if (x.from < (x.out ? end_any : end_out)) return PICASSO_ERR_INVALID_ARG;
+            end_any = std::max(end_any, x.to);
+            if (x.out) end_out = std::max(end_out, x.to);
+        }
+    }
+    hipStream_t s = (hipStream_t)stream;
+    ON_DEVICE(c);
+    double* ws = (double*)d_workspace;
+    const int partials = queue_squares(s, n, h_grads, h_sizes, h_types, ws);
+    bool first = true;
+    gradient_tables(n, h_grads, h_out, h_sizes, h_types, [&](const grads::Table& t, int groups) {
+        grads::scale_kernel<<<groups, feat::BLOCK, 0, s>>>(t, ws, partials, max_norm, first ? d_norm : nullptr);
+        first = false;
+    });
+    if (first && d_norm) grads::norm_kernel<<<1, feat::BLOCK, 0, s>>>(ws, 0, d_norm);  // (nothing to scale)
+    LAUNCHED(c);
+    return PICASSO_OK;
+}
+
+}  // extern "C"

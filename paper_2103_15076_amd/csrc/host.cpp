@@ -7,6 +7,8 @@
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
+#include <cmath>
+#include <string>
 #include <vector>
 
 #include "../../include/picasso.h"
@@ -376,6 +378,295 @@ PyObject* f2v_backward(Args& a) {
     return pack({wrap(gy), wrap(gw), want ? wrap(gpi) : none()});
 }
 
+// ---- operators on rows of features: their tensors may be of three types, and lie on the context's device
+
+// The call's context, device and stream (None: the device's current one).
+struct Where {
+    picasso_ctx* c;
+    int device;
+    PyObject* given;
+    void* s;
+    explicit Where(Args& a) : c(a.context()), device(a.i32()), given(a.next()) {
+        PyObject* number;
+        if (given == Py_None) {
+            PyObject* d = PyLong_FromLong(device);
+            if (!d) throw PyError{};
+            number = PyObject_CallOneArg(g_current_stream, d);
+            Py_DECREF(d);
+        } else {
+            number = PyObject_GetAttrString(given, "cuda_stream");
+        }
+        if (!number) throw PyError{};
+        s = PyLong_AsVoidPtr(number);
+        Py_DECREF(number);
+        if (PyErr_Occurred()) throw PyError{};
+    }
+    at::TensorOptions on() const { return at::TensorOptions().device(at::Device(at::kCUDA, (at::DeviceIndex)device)); }
+    // A tensor that this call allocates.  Used on a stream that the caller names, the allocator learns of it.
+    at::Tensor empty(at::IntArrayRef shape, at::ScalarType type) const {
+        at::Tensor t = at::empty(shape, on().dtype(type));
+        if (given != Py_None) {
+            PyObject* w = THPVariable_Wrap(t);
+            PyObject* r = w ? PyObject_CallMethod(w, "record_stream", "O", given) : nullptr;
+            Py_XDECREF(r);
+            Py_XDECREF(w);
+            if (!r) throw PyError{};
+        }
+        return t;
+    }
+    at::Tensor workspace(size_t bytes) const { return empty({(int64_t)std::max<size_t>(bytes, 16)}, at::kByte); }
+};
+
+[[noreturn]] void wrong(const char* what, const char* expected) {
+    PyErr_Format(PyExc_TypeError, "%s: expected %s", what, expected);
+    throw PyError{};
+}
+int type_of(const at::Tensor& t, const char* what) {
+    switch (t.scalar_type()) {
+        case at::kFloat: return PICASSO_F32;
+        case at::kBFloat16: return PICASSO_BF16;
+        case at::kHalf: return PICASSO_F16;
+        default: wrong(what, "a tensor of dtype torch.float32, torch.bfloat16 or torch.float16");
+    }
+}
+// A tensor on the context's device, or null for None where that is allowed.
+const at::Tensor* on_device(Args& a, const Where& w, const char* what, bool required) {
+    PyObject* o = a.next();
+    if (o == Py_None && !required) return nullptr;
+    if (!THPVariable_Check(o)) wrong(what, "a CUDA tensor");
+    const at::Tensor& t = THPVariable_Unpack(o);
+    if (!t.is_cuda() || t.get_device() != w.device) wrong(what, "a tensor on the context's CUDA device");
+    return &t;
+}
+// ... of this type and shape, contiguous
+const at::Tensor* exactly(Args& a, const Where& w, const char* what, at::ScalarType type, at::IntArrayRef shape, bool required) {
+    const at::Tensor* t = on_device(a, w, what, required);
+    if (t && (t->scalar_type() != type || t->sizes() != shape || !t->is_contiguous())) {
+        std::string s = "a contiguous tensor of dtype ";
+        s += at::toString(type);
+        s += " and shape (";
+        for (int64_t n : shape) s += std::to_string(n) + ",";
+        wrong(what, (s + ")").c_str());
+    }
+    return t;
+}
+void* data(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+int as_i32(int64_t n, const char* what) {
+    if (n > 0x7FFFFFFF) wrong(what, "less than 2^31 rows and columns");
+    return (int)n;
+}
+double number(Args& a) {
+    const double v = PyFloat_AsDouble(a.next());
+    if (v == -1.0 && PyErr_Occurred()) throw PyError{};
+    return v;
+}
+
+// Rows of features [N, C], contiguous.
+struct Features {
+    const at::Tensor& x;
+    int type, N, C;
+    Features(Args& a, const Where& w, const char* what) : x(*on_device(a, w, what, true)), type(type_of(x, what)) {
+        if (x.dim() != 2 || !x.is_contiguous()) wrong(what, "a contiguous tensor [rows, channels]");
+        N = as_i32(x.size(0), what);
+        C = as_i32(x.size(1), what);
+    }
+};
+
+PyObject* layer_norm_forward(Args& a) {
+    const Where w(a);
+    const Features f(a, w, "x");
+    const at::Tensor *gamma = exactly(a, w, "gamma", at::kFloat, {f.C}, false), *beta = exactly(a, w, "beta", at::kFloat, {f.C}, false);
+    const float eps = (float)number(a);
+    const at::Tensor* out = exactly(a, w, "out", f.x.scalar_type(), {f.N, f.C}, false);
+    const at::Tensor y = out ? *out : w.empty({f.N, f.C}, f.x.scalar_type()), mean = w.empty({f.N}, at::kFloat), rstd = w.empty({f.N}, at::kFloat);
+    checked(w.c, [&] {
+        return picasso_layer_norm_forward(w.c, w.s, f.type, f.x.data_ptr(), f.N, f.C, F(gamma), F(beta), eps, y.data_ptr(), F(mean), F(rstd));
+    });
+    return pack({wrap(y), wrap(mean), wrap(rstd)});
+}
+
+PyObject* layer_norm_backward(Args& a) {
+    const Where w(a);
+    const at::Tensor* gy = on_device(a, w, "gy", true);
+    const Features f(a, w, "x");
+    if (gy->scalar_type() != f.x.scalar_type() || gy->sizes() != f.x.sizes() || !gy->is_contiguous()) wrong("gy", "a contiguous tensor of x's dtype and shape");
+    const at::Tensor *gamma = exactly(a, w, "gamma", at::kFloat, {f.C}, false), *mean = exactly(a, w, "mean", at::kFloat, {f.N}, true),
+                     *rstd = exactly(a, w, "rstd", at::kFloat, {f.N}, true);
+    const size_t bytes = picasso_layer_norm_workspace_bytes(f.type, f.N, f.C);
+    const at::Tensor gx = w.empty({f.N, f.C}, f.x.scalar_type()), gg = w.empty({f.C}, at::kFloat), gb = w.empty({f.C}, at::kFloat), ws = w.workspace(bytes);
+    checked(w.c, [&] {
+        return picasso_layer_norm_backward(w.c, w.s, f.type, gy->data_ptr(), f.x.data_ptr(), f.N, f.C, F(gamma), F(mean), F(rstd), gx.data_ptr(),
+                                           F(gg), F(gb), ws.data_ptr(), bytes);
+    });
+    return pack({wrap(gx), wrap(gg), wrap(gb)});
+}
+
+// An array of heads [T, H, D], the features of a head next to each other.
+struct HeadsArg {
+    const at::Tensor* t;
+    picasso_heads h{};
+    HeadsArg(const at::Tensor* t_, const char* what) : t(t_) {
+        if (!t) return;
+        if (t->dim() != 3 || (t->size(2) > 1 && t->stride(2) != 1)) wrong(what, "a tensor [rows, heads, features] with its features next to each other");
+        // (the strides of an axis of one are arbitrary: replaced by what fits)
+        const int64_t head = t->size(1) > 1 ? t->stride(1) : t->size(2), row = t->size(0) > 1 ? t->stride(0) : std::max(t->size(1) * t->size(2), head);
+        h = picasso_heads{t->data_ptr(), row, head};
+    }
+    HeadsArg(Args& a, const Where& w, const char* what, bool required) : HeadsArg(on_device(a, w, what, required), what) {}
+};
+void alike(const HeadsArg& x, const char* what, at::ScalarType type, int64_t rows, int64_t heads, int64_t width) {
+    if (x.t->scalar_type() == type && x.t->size(0) == rows && x.t->size(1) == heads && x.t->size(2) == width) return;
+    PyErr_Format(PyExc_TypeError, "%s: expected a tensor of dtype %s and shape (%lld, %lld, %lld)", what, at::toString(type), (long long)rows,
+                 (long long)heads, (long long)width);
+    throw PyError{};
+}
+
+// q, k, v, their offsets, causal and the scale, which both passes take.
+struct AttentionArgs {
+    HeadsArg q, k, v;
+    at::ScalarType dtype;
+    int type, B, Tq, Tk, Hq, Hkv, D;
+    const at::Tensor *qo, *ko;
+    bool causal;
+    float scale;
+    AttentionArgs(Args& a, const Where& w) : q(a, w, "q", true), k(a, w, "k", true), v(a, w, "v", true) {
+        dtype = q.t->scalar_type();
+        type = type_of(*q.t, "q");
+        Tq = as_i32(q.t->size(0), "q"), Hq = as_i32(q.t->size(1), "q"), D = as_i32(q.t->size(2), "q");
+        Tk = as_i32(k.t->size(0), "k"), Hkv = as_i32(k.t->size(1), "k");
+        alike(k, "k", dtype, Tk, Hkv, D);
+        alike(v, "v", dtype, Tk, Hkv, D);
+        qo = on_device(a, w, "q_offsets", true);
+        if (qo->dim() != 1 || qo->size(0) < 2) wrong("q_offsets", "a contiguous tensor [sequences + 1] of dtype torch.int32");
+        B = as_i32(qo->size(0) - 1, "q_offsets");
+        ko = on_device(a, w, "k_offsets", false);
+        for (const at::Tensor* o : {qo, ko})
+            if (o && (o->scalar_type() != at::kInt || !o->is_contiguous() || o->dim() != 1 || o->size(0) != B + 1))
+                wrong(o == qo ? "q_offsets" : "k_offsets", "a contiguous tensor [sequences + 1] of dtype torch.int32");
+        if (!ko) {
+            if (Tq != Tk) wrong("k_offsets", "offsets of the keys, whose number is not the queries'");
+            ko = qo;
+        }
+        causal = a.i32() != 0;
+        PyObject* s = a.next();
+        if (s == Py_None) {
+            scale = D > 0 ? (float)(1.0 / std::sqrt((double)D)) : 0.0f;
+        } else {
+            scale = (float)PyFloat_AsDouble(s);
+            if (PyErr_Occurred()) throw PyError{};
+        }
+    }
+};
+
+PyObject* attention_forward(Args& a) {
+    const Where w(a);
+    const AttentionArgs x(a, w);
+    const HeadsArg given(a, w, "out", false);
+    if (given.t) alike(given, "out", x.dtype, x.Tq, x.Hq, x.D);
+    const at::Tensor o = given.t ? *given.t : w.empty({x.Tq, x.Hq, x.D}, x.dtype), lse = w.empty({x.Hq, x.Tq}, at::kFloat);
+    const HeadsArg out(&o, "out");
+    const size_t bytes = picasso_attention_workspace_bytes(x.type, x.B, x.Tq, x.Tk, x.Hq, x.Hkv, x.D, 0);
+    const at::Tensor ws = bytes ? w.workspace(bytes) : at::Tensor();
+    checked(w.c, [&] {
+        // (what this call allocates has no rows to leave as they were: those of no sequence are cleared)
+        return picasso_attention_forward(w.c, w.s, x.type, &x.q.h, &x.k.h, &x.v.h, I(x.qo), I(x.ko), x.B, x.Tq, x.Tk, x.Hq, x.Hkv, x.D, x.causal,
+                                         x.scale, given.t == nullptr, &out.h, F(lse), bytes ? ws.data_ptr() : nullptr, bytes);
+    });
+    return pack({wrap(o), wrap(lse)});
+}
+
+PyObject* attention_backward(Args& a) {
+    const Where w(a);
+    const HeadsArg gout(a, w, "gout", true);
+    const AttentionArgs x(a, w);
+    const HeadsArg out(a, w, "out", true);
+    alike(gout, "gout", x.dtype, x.Tq, x.Hq, x.D);
+    alike(out, "out", x.dtype, x.Tq, x.Hq, x.D);
+    const at::Tensor* lse = exactly(a, w, "lse", at::kFloat, {x.Hq, x.Tq}, true);
+    const HeadsArg to_q(a, w, "gq", false), to_k(a, w, "gk", false), to_v(a, w, "gv", false);
+    const bool given = to_q.t || to_k.t || to_v.t;
+    if (given && !(to_q.t && to_k.t && to_v.t)) wrong("out", "all three gradients' tensors or none");
+    if (given) {
+        alike(to_q, "gq", x.dtype, x.Tq, x.Hq, x.D);
+        alike(to_k, "gk", x.dtype, x.Tk, x.Hkv, x.D);
+        alike(to_v, "gv", x.dtype, x.Tk, x.Hkv, x.D);
+    }
+    const at::Tensor tq = given ? *to_q.t : w.empty({x.Tq, x.Hq, x.D}, x.dtype), tk = given ? *to_k.t : w.empty({x.Tk, x.Hkv, x.D}, x.dtype),
+                     tv = given ? *to_v.t : w.empty({x.Tk, x.Hkv, x.D}, x.dtype);
+    const HeadsArg gq(&tq, "gq"), gk(&tk, "gk"), gv(&tv, "gv");
+    const size_t bytes = picasso_attention_workspace_bytes(x.type, x.B, x.Tq, x.Tk, x.Hq, x.Hkv, x.D, 1);
+    const at::Tensor ws = w.workspace(bytes);
+    checked(w.c, [&] {
+        return picasso_attention_backward(w.c, w.s, x.type, &gout.h, &x.q.h, &x.k.h, &x.v.h, &out.h, F(lse), I(x.qo), I(x.ko), x.B, x.Tq, x.Tk, x.Hq,
+                                          x.Hkv, x.D, x.causal, x.scale, !given, &gq.h, &gk.h, &gv.h, ws.data_ptr(), bytes);
+    });
+    return pack({wrap(tq), wrap(tk), wrap(tv)});
+}
+
+// A sequence of contiguous tensors on the context's device, of any shapes.
+struct Tensors {
+    PyObject* seq;
+    std::vector<const void*> data;
+    std::vector<int64_t> sizes;
+    std::vector<int32_t> types;
+    Tensors(PyObject* o, const Where& w, const char* what) : seq(PySequence_Fast(o, "expected a sequence of tensors")) {
+        if (!seq) throw PyError{};
+        try {
+            const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
+            data.reserve(n), sizes.reserve(n), types.reserve(n);
+            for (Py_ssize_t k = 0; k < n; ++k) {
+                PyObject* item = PySequence_Fast_ITEMS(seq)[k];
+                if (!THPVariable_Check(item)) wrong(what, "a sequence of tensors");
+                const at::Tensor& t = THPVariable_Unpack(item);
+                if (!t.is_cuda() || t.get_device() != w.device || !t.is_contiguous()) wrong(what, "contiguous tensors on the context's CUDA device");
+                types.push_back(type_of(t, what));
+                data.push_back(t.data_ptr());
+                sizes.push_back(t.numel());
+            }
+        } catch (...) {
+            Py_DECREF(seq);
+            throw;
+        }
+    }
+    ~Tensors() { Py_DECREF(seq); }
+    Tensors(const Tensors&) = delete;
+    int n() const { return (int)data.size(); }
+};
+
+PyObject* gradient_norm(Args& a) {
+    const Where w(a);
+    const Tensors g(a.next(), w, "grads");
+    const size_t bytes = picasso_gradients_workspace_bytes(g.n(), g.sizes.data());
+    const at::Tensor norm = w.empty({1}, at::kFloat), ws = w.workspace(bytes);
+    checked(w.c, [&] {
+        return picasso_gradient_norm(w.c, w.s, g.n(), g.data.data(), g.sizes.data(), g.types.data(), F(norm), ws.data_ptr(), bytes);
+    });
+    return wrap(norm);
+}
+
+PyObject* clip_gradients(Args& a) {
+    const Where w(a);
+    const Tensors g(a.next(), w, "grads");
+    const double max_norm = number(a);
+    PyObject* o = a.next();
+    std::vector<void*> to;
+    to.reserve(g.n());
+    if (o == Py_None) {
+        for (const void* p : g.data) to.push_back(const_cast<void*>(p));
+    } else {
+        const Tensors out(o, w, "out");
+        if (out.sizes != g.sizes || out.types != g.types) wrong("out", "tensors of the gradients' dtypes and sizes");
+        for (const void* p : out.data) to.push_back(const_cast<void*>(p));
+    }
+    const size_t bytes = picasso_gradients_workspace_bytes(g.n(), g.sizes.data());
+    const at::Tensor norm = w.empty({1}, at::kFloat), ws = w.workspace(bytes);
+    checked(w.c, [&] {
+        return picasso_clip_gradients(w.c, w.s, g.n(), g.data.data(), g.sizes.data(), g.types.data(), max_norm, to.data(), F(norm), ws.data_ptr(),
+                                      bytes);
+    });
+    return wrap(norm);
+}
+
 // (current_device, current_stream, raise): the callables above
 PyObject* set_callbacks(Args& a) {
     for (PyObject** p : {&g_current_device, &g_current_stream, &g_raise}) {
@@ -393,7 +684,9 @@ PyMethodDef methods[] = {
     PICASSO_ENTRY(pool_backward), PICASSO_ENTRY(unpool_forward), PICASSO_ENTRY(unpool_backward),
     PICASSO_ENTRY(vertex_corner_csr), PICASSO_ENTRY(facet_geometry), PICASSO_ENTRY(fuzzy_coefficients),
     PICASSO_ENTRY(v2f_forward), PICASSO_ENTRY(v2f_backward), PICASSO_ENTRY(f2f_forward), PICASSO_ENTRY(f2f_backward),
-    PICASSO_ENTRY(f2v_forward), PICASSO_ENTRY(f2v_backward), PICASSO_ENTRY(set_callbacks), {nullptr, nullptr, 0, nullptr}};
+    PICASSO_ENTRY(f2v_forward), PICASSO_ENTRY(f2v_backward), PICASSO_ENTRY(layer_norm_forward), PICASSO_ENTRY(layer_norm_backward),
+    PICASSO_ENTRY(attention_forward), PICASSO_ENTRY(attention_backward), PICASSO_ENTRY(gradient_norm), PICASSO_ENTRY(clip_gradients),
+    PICASSO_ENTRY(set_callbacks), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_host", "calls of include/picasso.h on torch tensors", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -16,6 +16,7 @@
 #include <new>
 
 #include "../../include/picasso.h"
+#include "context.h"
 #include "primitives.h"
 #include "decimate_kernels.h"
 #include "pooling.h"
@@ -1695,6 +1696,9 @@ std::atomic<int*> scratch_ptr[STATIC_MAX_DEVICES];  // per device: where its cop
 // ---------------------------------------------------------------------------
 // C-ABI
 // ---------------------------------------------------------------------------
+int picasso_device_of(const picasso_ctx* c) { return c->device; }
+void picasso_note_hip_error(picasso_ctx* c, const char* text) { snprintf(c->hip_err, sizeof(c->hip_err), "%s", text); }
+
 extern "C" {
 
 size_t picasso_workspace_bytes(int64_t max_verts, int64_t max_facets, int32_t max_meshes) {
