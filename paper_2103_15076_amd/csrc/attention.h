@@ -196,18 +196,21 @@ struct Staged {
     static constexpr int CHUNKS = Rows<T, DP>::CHUNKS, V = Rows<T, DP>::V, N = (ROWS * CHUNKS + BLOCK - 1) / BLOCK;
     static constexpr bool EVEN = ROWS * CHUNKS % BLOCK == 0;
     Quad q[N];
-    // row(r): address of row r of the tile, or null where there is none; D: features
+    // row(r): address of row r of the tile, of which the first `rows` (one at least) are there; the others, and features behind
+    // the D-th, become 0.  Loads are not conditional (those of no row take the last's), so that all are in flight together.
     template <typename Row>
-    __device__ __forceinline__ void load(int D, Row row) {
+    __device__ __forceinline__ void load(int D, int rows, Row row) {
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             const int u = (int)threadIdx.x + i * BLOCK, r = u / CHUNKS, c = u % CHUNKS;
-            Quad v = {0, 0, 0, 0};
-            if ((EVEN || r < ROWS) && c * V < D) {
-                const T* p = row(r);
-                if (p) v = *reinterpret_cast<const Quad*>(p + c * V);
+            q[i] = *reinterpret_cast<const Quad*>(row(r < rows ? r : rows - 1) + (c * V < D ? c * V : 0));
+        }
+        if (rows < ROWS || D < DP) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const int u = (int)threadIdx.x + i * BLOCK, r = u / CHUNKS, c = u % CHUNKS;
+                if (r >= rows || c * V >= D) q[i] = Quad{0, 0, 0, 0};
             }
-            q[i] = v;
         }
     }
     __device__ __forceinline__ void store(T* tile) const {
@@ -330,7 +333,7 @@ struct Scale {
 };
 
 template <typename T, int DP, int ROW_WAVES>
-__global__ __launch_bounds__(BLOCK) void forward_kernel(Heads<const T> q, Heads<const T> k, Heads<const T> v, Offsets off, int Hq,
+__global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || DP <= 64 ? 2 : 1) void forward_kernel(Heads<const T> q, Heads<const T> k, Heads<const T> v, Offsets off, int Hq,
                                                         int Hkv, Group group, int D, int causal, int clear, float scale2, Heads<T> out,
                                                         float* __restrict__ lse, float* __restrict__ part_out,
                                                         float* __restrict__ part_lse) {
@@ -374,8 +377,8 @@ __global__ __launch_bounds__(BLOCK) void forward_kernel(Heads<const T> q, Heads<
     const T* const kp = k.p + (size_t)k_start * k.row + (size_t)kvh * k.head;
     const T* const vp = v.p + (size_t)k_start * v.row + (size_t)kvh * v.head;
     auto fetch = [&](int j0) {
-        sk.load(D, [&](int r) { return j0 + r < k_end ? kp + (size_t)(j0 + r) * k.row : nullptr; });
-        sv.load(D, [&](int r) { return j0 + r < k_end ? vp + (size_t)(j0 + r) * v.row : nullptr; });
+        sk.load(D, k_end - j0, [&](int r) { return kp + (size_t)(j0 + r) * k.row; });
+        sv.load(D, k_end - j0, [&](int r) { return vp + (size_t)(j0 + r) * v.row; });
     };
     if (k_begin < k_end) fetch(k_begin);
     int buffer = 0;
@@ -558,10 +561,13 @@ template <typename T, int DP>
 struct KeysShape {
     static constexpr int KEYS = 128, ROWS = 32;
     static constexpr int TILE = ROWS * DP;
+    // 16-bit rows of 128: a lane's key and value, two accumulators and two products are more than the 256 registers of two waves a
+    // SIMD; the values go to LDS
+    static constexpr bool VALUES_IN_LDS = sizeof(T) == 2 && DP == 128;
     static constexpr int BUFFERS = 4 * TILE * (int)sizeof(T) <= 80 * 1024 ? 2 : 1;
 };
 template <typename T, int DP>
-__global__ __launch_bounds__(BLOCK) void backward_keys_kernel(Heads<const T> gout, Heads<const T> q, Heads<const T> k, Heads<const T> v,
+__global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || DP <= 64 ? 2 : 1) void backward_keys_kernel(Heads<const T> gout, Heads<const T> q, Heads<const T> k, Heads<const T> v,
                                                               const float* __restrict__ lse, const float* __restrict__ delta,
                                                               Offsets off, int Hq, int Hkv, Group group, int D, int causal, int clear, Scale scale,
                                                               Heads<T> gk, Heads<T> gv, float* __restrict__ part_k,
@@ -570,6 +576,7 @@ __global__ __launch_bounds__(BLOCK) void backward_keys_kernel(Heads<const T> gou
     constexpr int DB = DP / 32;
     __shared__ __attribute__((aligned(16))) T lds[S::BUFFERS * 2 * S::TILE];
     __shared__ __attribute__((aligned(16))) float stat[S::BUFFERS][2][S::ROWS];
+    __shared__ __attribute__((aligned(16))) T own_v[S::VALUES_IN_LDS ? S::KEYS * DP : 8];
     const int G = group.G, kvh = blockIdx.y, split = blockIdx.z, splits = gridDim.z;
     const Tile t = find_tile<S::KEYS>(off.k, off.B, off.Tk, 1, blockIdx.x);
     if (!t.on || (t.seq < 0 && !clear)) return;
@@ -596,6 +603,11 @@ __global__ __launch_bounds__(BLOCK) void backward_keys_kernel(Heads<const T> gou
     const bool any = key_on && r_begin < r_end;
     own_row<T, DP>(any ? k.p + (size_t)(t.start + key) * k.row + (size_t)kvh * k.head : nullptr, D, half, fk);
     own_row<T, DP>(any ? v.p + (size_t)(t.start + key) * v.row + (size_t)kvh * v.head : nullptr, D, half, fv);
+    if constexpr (S::VALUES_IN_LDS) {  // (read by the wave that writes them)
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s)
+            *reinterpret_cast<Frag<T>*>(own_v + Rows<T, DP>::at(32 * wave + (lane & 31), 2 * s + half)) = fv[s];
+    }
     Acc ak[DB], av[DB];
 #pragma unroll
     for (int db = 0; db < DB; ++db) {
@@ -614,13 +626,15 @@ __global__ __launch_bounds__(BLOCK) void backward_keys_kernel(Heads<const T> gou
             *head = kvh * G + row - i * G;
             return row < r_end;
         };
-        sq.load(D, [&](int r) -> const T* {
+        sq.load(D, r_end - r0, [&](int r) {
             int tk, hd;
-            return place(r, &tk, &hd) ? q.p + (size_t)tk * q.row + (size_t)hd * q.head : nullptr;
+            place(r, &tk, &hd);
+            return q.p + (size_t)tk * q.row + (size_t)hd * q.head;
         });
-        sg.load(D, [&](int r) -> const T* {
+        sg.load(D, r_end - r0, [&](int r) {
             int tk, hd;
-            return place(r, &tk, &hd) ? gout.p + (size_t)tk * gout.row + (size_t)hd * gout.head : nullptr;
+            place(r, &tk, &hd);
+            return gout.p + (size_t)tk * gout.row + (size_t)hd * gout.head;
         });
         if ((int)threadIdx.x < 2 * S::ROWS) {
             int tk, hd;
@@ -652,7 +666,8 @@ __global__ __launch_bounds__(BLOCK) void backward_keys_kernel(Heads<const T> gou
 #pragma unroll
         for (int d = 0; d < DP / 16; ++d) {
             p = Types<T>::mfma(Rows<T, DP>::along(tq, lane & 31, d, half), fk[d], p);
-            ds = Types<T>::mfma(Rows<T, DP>::along(tg, lane & 31, d, half), fv[d], ds);
+            const Frag<T> value = S::VALUES_IN_LDS ? Rows<T, DP>::along(own_v, 32 * wave + (lane & 31), d, half) : fv[d];
+            ds = Types<T>::mfma(Rows<T, DP>::along(tg, lane & 31, d, half), value, ds);
         }
         const bool border = causal && t.first + S::KEYS - 1 > group.query(r0) + shift;
 #pragma unroll
@@ -663,14 +678,16 @@ __global__ __launch_bounds__(BLOCK) void backward_keys_kernel(Heads<const T> gou
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int r = 4 * g + i;
-                float x = __builtin_amdgcn_exp2f(fmaf(p[r], scale.log2, -l4[i]));
-                float y = x * (ds[r] - d4[i]);  // (raised as x is)
-                if (border && key > group.query(r0 + 8 * g + 4 * half + i) + shift) {
-                    x = 0.0f;
-                    y = 0.0f;
-                }
-                p[r] = x;
-                ds[r] = y;
+                p[r] = __builtin_amdgcn_exp2f(fmaf(p[r], scale.log2, -l4[i]));
+                ds[r] = p[r] * (ds[r] - d4[i]);  // (raised as p is)
+            }
+        }
+        if (border) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+                const bool hidden = key > group.query(r0 + acc_row(r) + 4 * half) + shift;
+                p[r] = hidden ? 0.0f : p[r];
+                ds[r] = hidden ? 0.0f : ds[r];
             }
         }
         range.fit(ds, ak);
@@ -706,7 +723,7 @@ struct QueriesShape {
     static constexpr int BUFFERS = 4 * TILE * (int)sizeof(T) <= 80 * 1024 ? 2 : 1;
 };
 template <typename T, int DP>
-__global__ __launch_bounds__(BLOCK) void backward_queries_kernel(Heads<const T> gout, Heads<const T> q, Heads<const T> k,
+__global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || DP <= 64 ? 2 : 1) void backward_queries_kernel(Heads<const T> gout, Heads<const T> q, Heads<const T> k,
                                                                  Heads<const T> v, const float* __restrict__ lse,
                                                                  const float* __restrict__ delta, Offsets off, int Hq, int Hkv, Group group, int D,
                                                                  int causal, int clear, Scale scale, Heads<T> gq,
@@ -755,8 +772,8 @@ __global__ __launch_bounds__(BLOCK) void backward_queries_kernel(Heads<const T> 
     const T* const kp = k.p + (size_t)k_start * k.row + (size_t)kvh * k.head;
     const T* const vp = v.p + (size_t)k_start * v.row + (size_t)kvh * v.head;
     auto fetch = [&](int j0) {
-        sk.load(D, [&](int r) { return j0 + r < k_end ? kp + (size_t)(j0 + r) * k.row : nullptr; });
-        sv.load(D, [&](int r) { return j0 + r < k_end ? vp + (size_t)(j0 + r) * v.row : nullptr; });
+        sk.load(D, k_end - j0, [&](int r) { return kp + (size_t)(j0 + r) * k.row; });
+        sv.load(D, k_end - j0, [&](int r) { return vp + (size_t)(j0 + r) * v.row; });
     };
     if (k_begin < k_end) fetch(k_begin);
     int buffer = 0;
@@ -781,7 +798,10 @@ __global__ __launch_bounds__(BLOCK) void backward_queries_kernel(Heads<const T> 
         for (int r = 0; r < 16; ++r) {
             const float x = __builtin_amdgcn_exp2f(fmaf(p[r], scale.log2, -ls));
             ds[r] = x * (ds[r] - dl);
-            if (border && j0 + acc_row(r) + 4 * half >= seen) ds[r] = 0.0f;
+        }
+        if (border) {
+#pragma unroll
+            for (int r = 0; r < 16; ++r) ds[r] = j0 + acc_row(r) + 4 * half >= seen ? 0.0f : ds[r];
         }
         range.fit(ds, &acc[0]);
 #pragma unroll

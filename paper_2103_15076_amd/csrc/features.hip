@@ -5,6 +5,7 @@
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
+#include <stdlib.h>
 
 #include <algorithm>
 #include <vector>
@@ -180,7 +181,9 @@ ForwardPlan forward_plan(const Attention& a) {
     // short sequences and single tokens: 32 rows a workgroup, and too few groups of 128 to fill the chip
     p.row_waves = a.rows() <= 48ll * a.B || groups128 < 256 ? 1 : 4;
     const long long groups = p.row_waves == 4 ? groups128 : (a.rows() / 32 + a.B) * a.Hkv;
+    if (getenv("PK_RW")) p.row_waves = atoi(getenv("PK_RW"));
     p.splits = splits_for(groups, keys, 256);
+    if (getenv("PK_FS")) p.splits = atoi(getenv("PK_FS"));
     return p;
 }
 struct BackwardPlan {
@@ -190,6 +193,8 @@ BackwardPlan backward_plan(const Attention& a) {
     BackwardPlan p;
     p.key_splits = splits_for(((long long)a.Tk / 128 + a.B) * a.Hkv, a.rows() / a.B, 128);
     p.query_splits = splits_for((a.rows() / 128 + a.B) * a.Hkv, a.Tk / a.B, 128);
+    if (getenv("PK_KS")) p.key_splits = atoi(getenv("PK_KS"));
+    if (getenv("PK_QS")) p.query_splits = atoi(getenv("PK_QS"));
     return p;
 }
 
