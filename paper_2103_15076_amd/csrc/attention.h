@@ -23,7 +23,7 @@
 // Rounding: scores, statistics and all sums are binary32.  For 16-bit features the probabilities and ds are rounded to the
 // features' type, as the matrix instructions take them: half a step each, relative, of terms of a sum whose result is rounded
 // to the same type.  binary16 has few exponents (a weight of one of a hundred thousand keys is below its normal range), so there
-// the probabilities are carried times 2^15 and ds times a power of two that keeps a wave's largest within the range (Range).
+// the probabilities are carried times 2^15 and ds times a power of two that keeps a key's or query's largest within the range (Range).
 #pragma once
 #include <type_traits>
 
@@ -275,8 +275,10 @@ __device__ __forceinline__ void store_own_row(T* p, int D, int half, const Acc* 
 template <typename T>
 constexpr float RAISE = std::is_same_v<T, feat::f16> ? 15.0f : 0.0f;
 
-// The power of two that a wave carries ds by: lowered, and the accumulators with it, when a value would leave binary16's range;
-// nothing for the other types.  It settles within the first few tiles.
+// The power of two that a lane carries ds by: lowered, and the lane's accumulators with it, when a value would leave binary16's
+// range; nothing for the other types.  A lane's ds all belong to one key (or query), as its accumulators do, half of them in the
+// lane of the other half: each key has a power of its own, and what another lane holds (nothing, where there is no key) is nothing to it.
+// It settles within the first few tiles.
 template <typename T, int DB>
 struct Range {
     float by = std::is_same_v<T, feat::f16> ? 0x1p40f : 1.0f;
@@ -286,9 +288,9 @@ struct Range {
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, fabsf(ds[r]));
             if (__ballot(most * by > 0x1p15f)) {
-                most = feat::over_lanes<Most, 64>(most);
+                most = over_halves<Most>(most);
                 // most < 2^e: by 2^(15 - e) it stays below 2^15.  (Infinite: whatever it is carried by)
-                const float to = most < INFINITY ? ldexpf(1.0f, 15 - min(ilogbf(most) + 1, 120)) : by;
+                const float to = most * by > 0x1p15f && most < INFINITY ? ldexpf(1.0f, 15 - min(ilogbf(most) + 1, 120)) : by;
                 const float f = to / by;
 #pragma unroll
                 for (int db = 0; db < DB; ++db)

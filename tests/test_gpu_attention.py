@@ -314,3 +314,53 @@ def test_refusals(ctx):
             f()
             print("not refused:", n)
         assert e.value.status == pk.PICASSO_ERR_INVALID_ARG
+
+
+def shifted(lq, lk, hq, hkv, d, seed, by):
+    """Inputs whose scores (times 1 / sqrt(d)) all have `by` < 0 added: feature 0 is of one size and opposite signs in q and k."""
+    q, k, v, go = make(lq, lk, hq, hkv, d, "f16", seed)
+    a = math.sqrt(-by * math.sqrt(d))
+    q[..., 0], k[..., 0] = a, -a
+    return q, k, v, go
+
+
+@pytest.mark.parametrize("by", [-5.0, -30.0, -60.0, -95.0])
+@pytest.mark.parametrize("lq,lk,heads,d", [([32], [40], (1, 1), 32), ([70, 33], [1, 97], (2, 1), 64), ([45], [130], (2, 2), 128), ([40], [2100], (1, 1), 32)])
+def test_float16_keys_behind_the_last_do_not_weigh(ctx, lq, lk, heads, d, by):
+    """All scores far below 0 and a number of keys that no tile is a multiple of: what lanes without a key hold (a score of 0) is no
+    weight of anything, and the gradients of the keys beside them are held to the bars."""
+    print(f"attention f16 lq={lq} lk={lk} {heads} d={d} shifted by {by}", flush=True)
+    q, k, v, go = shifted(lq, lk, *heads, d, 5, by)
+    qo, ko = offsets(lq), offsets(lk)
+    out, lse = ctx.picasso_attention_forward(q, k, v, qo, ko)
+    g = ctx.picasso_attention_backward(go, q, k, v, out, lse, qo, ko)
+    want = reference(q, k, v, go, lq, lk, False, 1 / math.sqrt(d), torch.finfo(torch.float16).eps / 2, small=True)
+    for name, got in zip(("out", "lse", "gq", "gk", "gv"), (out, lse) + g):
+        value, bar = want[name]
+        held(got, (value, bar + (2.0 ** -25 if name != "lse" else 0.0)), name)
+
+
+def test_float16_gradients_of_far_sizes_side_by_side(ctx):
+    """Every second key has weights near 2^-27 beside keys that share the rest: gradients from 2^13 down to 2^-14, neighbours in one
+    tile, each within its own bar: ds, carried by a power of two that puts the largest of a key (of gk; of a query, of gq) between 2^13 and
+    2^15, is off by 2^-38 of the largest of that key or query."""
+    n, m, d = 40, 44, 32
+    scale = 1 / math.sqrt(d)
+    q, k, v, go = make([n], [m], 1, 1, d, "f16", 11)
+    q, v, go = q * 2.0 ** -2, v * 2.0 ** 7, go * 2.0 ** 7
+    q[..., 0] = 2.0 ** -4
+    k[..., 0] = 0.0
+    k[1::2, :, 0] = -27 * math.log(2) / (scale * 2.0 ** -4)
+    o1, o2 = offsets([n]), offsets([m])
+    out, lse = ctx.picasso_attention_forward(q, k, v, o1, o2)
+    gq, gk, gv = ctx.picasso_attention_backward(go, q, k, v, out, lse, o1, o2)
+    want = reference(q, k, v, go, [n], [m], False, scale, torch.finfo(torch.float16).eps / 2)
+    Q, K, V, O = (t[:, 0].double().cpu() for t in (q, k, v, go))
+    p = torch.softmax(scale * Q @ K.T, 1)
+    dp = O @ V.T
+    ds = p * (dp - (p * dp).sum(1, keepdim=True))
+    value, bar = want["gk"]
+    assert value[0::2].abs().max() > 2.0 ** 8 and value[1::2].abs().max() < 2.0 ** -12 and (value[1::2].abs() > 2.0 ** -24).any()
+    held(gk, (value, bar + scale * 2.0 ** -38 * (ds.abs().amax(0)[:, None] * Q.abs().sum(0))[:, None] + 2.0 ** -25), "gk")
+    value, bar = want["gq"]
+    held(gq, (value, bar + scale * 2.0 ** -38 * (ds.abs().amax(1)[:, None] * K.abs().sum(0))[:, None] + 2.0 ** -25), "gq")
