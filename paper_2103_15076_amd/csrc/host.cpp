@@ -8,6 +8,7 @@
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
+#include <optional>
 #include <string>
 #include <vector>
 
@@ -603,22 +604,26 @@ PyObject* attention_backward(Args& a) {
     return pack({wrap(tq), wrap(tk), wrap(tv)});
 }
 
-// A sequence of contiguous tensors on the context's device, of any shapes.
+// A sequence of contiguous tensors on the context's device, of any shapes.  They live as long as this does, until the kernels are
+// queued, whatever becomes of the sequence: a generator's may have no other owner, and another thread may change a list.  (What
+// is allocated meanwhile must not get their memory.)
 struct Tensors {
-    PyObject* seq;
+    std::vector<at::Tensor> held;
     std::vector<const void*> data;
     std::vector<int64_t> sizes;
     std::vector<int32_t> types;
-    Tensors(PyObject* o, const Where& w, const char* what) : seq(PySequence_Fast(o, "expected a sequence of tensors")) {
+    Tensors(PyObject* o, const Where& w, const char* what) {
+        PyObject* seq = PySequence_Fast(o, "expected a sequence of tensors");
         if (!seq) throw PyError{};
         try {
             const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
-            data.reserve(n), sizes.reserve(n), types.reserve(n);
+            held.reserve(n), data.reserve(n), sizes.reserve(n), types.reserve(n);
             for (Py_ssize_t k = 0; k < n; ++k) {
                 PyObject* item = PySequence_Fast_ITEMS(seq)[k];
                 if (!THPVariable_Check(item)) wrong(what, "a sequence of tensors");
                 const at::Tensor& t = THPVariable_Unpack(item);
                 if (!t.is_cuda() || t.get_device() != w.device || !t.is_contiguous()) wrong(what, "contiguous tensors on the context's CUDA device");
+                held.push_back(t);
                 types.push_back(type_of(t, what));
                 data.push_back(t.data_ptr());
                 sizes.push_back(t.numel());
@@ -627,9 +632,8 @@ struct Tensors {
             Py_DECREF(seq);
             throw;
         }
+        Py_DECREF(seq);
     }
-    ~Tensors() { Py_DECREF(seq); }
-    Tensors(const Tensors&) = delete;
     int n() const { return (int)data.size(); }
 };
 
@@ -649,15 +653,12 @@ PyObject* clip_gradients(Args& a) {
     const Tensors g(a.next(), w, "grads");
     const double max_norm = number(a);
     PyObject* o = a.next();
+    std::optional<Tensors> out;
+    if (o != Py_None) out.emplace(o, w, "out");
+    if (out && (out->sizes != g.sizes || out->types != g.types)) wrong("out", "tensors of the gradients' dtypes and sizes");
     std::vector<void*> to;
     to.reserve(g.n());
-    if (o == Py_None) {
-        for (const void* p : g.data) to.push_back(const_cast<void*>(p));
-    } else {
-        const Tensors out(o, w, "out");
-        if (out.sizes != g.sizes || out.types != g.types) wrong("out", "tensors of the gradients' dtypes and sizes");
-        for (const void* p : out.data) to.push_back(const_cast<void*>(p));
-    }
+    for (const void* p : out ? out->data : g.data) to.push_back(const_cast<void*>(p));
     const size_t bytes = picasso_gradients_workspace_bytes(g.n(), g.sizes.data());
     const at::Tensor norm = w.empty({1}, at::kFloat), ws = w.workspace(bytes);
     checked(w.c, [&] {

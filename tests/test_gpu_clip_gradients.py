@@ -128,3 +128,22 @@ def test_refusals(ctx):
         assert e.value.status == pk.PICASSO_ERR_INVALID_ARG
     assert (a == 1).all() and (flat == 1).all()
     assert abs(float(ctx.picasso_gradient_norm([a, a])) - math.sqrt(20)) < 1e-5   # (read only: counted twice)
+
+
+def test_tensors_that_only_a_generator_makes(ctx):
+    """Outputs (and gradients) that nothing but the call holds: what the call allocates itself, the norm and the partial sums, is not laid
+    into their memory.  (Sizes as of the norm's own block and of larger ones.)"""
+    for n in (1, 100, 3000, 300_000):
+        g = tensors([n, n, n], [F32], n)
+        want = math.sqrt(sum(float((t.double() ** 2).sum()) for t in g))
+        for _ in range(3):
+            norm = ctx.picasso_clip_gradients(g, 0.25, out=(torch.empty_like(t) for t in g))
+            assert abs(float(norm) - want) <= (U + 1e-12) * want, n
+            norm = ctx.picasso_clip_gradients((t.clone() for t in g), 0.25)
+            assert abs(float(norm) - want) <= (U + 1e-12) * want, n
+            assert abs(float(ctx.picasso_gradient_norm(map(torch.clone, g))) - want) <= (U + 1e-12) * want, n
+    out = [torch.empty_like(t) for t in g]
+    ctx.picasso_clip_gradients(iter(g), 0.25, out=(t.view(-1) for t in out))
+    for t, o in zip(g, out):
+        w = min(1.0, 0.25 / (want + 1e-6)) * t.double()
+        assert ((o.double() - w).abs() <= 2.002 * U * w.abs() + 2.0 ** -149).all()
