@@ -5,7 +5,6 @@
 #include <math.h>
 #include <stdint.h>
 #include <stdio.h>
-#include <stdlib.h>
 
 #include <algorithm>
 #include <vector>
@@ -181,9 +180,7 @@ ForwardPlan forward_plan(const Attention& a) {
     // short sequences and single tokens: 32 rows a workgroup, and too few groups of 128 to fill the chip
     p.row_waves = a.rows() <= 48ll * a.B || groups128 < 256 ? 1 : 4;
     const long long groups = p.row_waves == 4 ? groups128 : (a.rows() / 32 + a.B) * a.Hkv;
-    if (getenv("PK_RW")) p.row_waves = atoi(getenv("PK_RW"));
     p.splits = splits_for(groups, keys, 256);
-    if (getenv("PK_FS")) p.splits = atoi(getenv("PK_FS"));
     return p;
 }
 struct BackwardPlan {
@@ -193,18 +190,14 @@ BackwardPlan backward_plan(const Attention& a) {
     BackwardPlan p;
     p.key_splits = splits_for(((long long)a.Tk / 128 + a.B) * a.Hkv, a.rows() / a.B, 128);
     p.query_splits = splits_for((a.rows() / 128 + a.B) * a.Hkv, a.Tk / a.B, 128);
-    if (getenv("PK_KS")) p.key_splits = atoi(getenv("PK_KS"));
-    if (getenv("PK_QS")) p.query_splits = atoi(getenv("PK_QS"));
     return p;
 }
 
-size_t attention_forward_bytes(const Attention& a) {
-    const ForwardPlan p = forward_plan(a);
+size_t attention_forward_bytes(const Attention& a, const ForwardPlan& p) {
     if (p.splits == 1) return 0;
     return up((size_t)p.splits * a.Tq * a.Hq * a.D * 4) + up((size_t)p.splits * a.Tq * a.Hq * 4);
 }
-size_t attention_backward_bytes(const Attention& a) {
-    const BackwardPlan p = backward_plan(a);
+size_t attention_backward_bytes(const Attention& a, const BackwardPlan& p) {
     const size_t keys = p.key_splits == 1 ? 0 : 2 * up((size_t)p.key_splits * a.Tk * a.Hkv * a.D * 4);
     const size_t queries = p.query_splits == 1 ? 0 : up((size_t)p.query_splits * a.Tq * a.Hq * a.D * 4);
     return up((size_t)a.Tq * a.Hq * 4) + std::max(keys, queries);
@@ -337,7 +330,7 @@ int picasso_layer_norm_backward(picasso_ctx* c, void* stream, int type, const vo
 size_t picasso_attention_workspace_bytes(int type, int32_t B, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv, int32_t D, int backward) {
     const Attention a{type, B, Tq, Tk, Hq, Hkv, D};
     if (!valid(a)) return 0;
-    return backward ? attention_backward_bytes(a) : attention_forward_bytes(a);
+    return backward ? attention_backward_bytes(a, backward_plan(a)) : attention_forward_bytes(a, forward_plan(a));
 }
 
 int picasso_attention_forward(picasso_ctx* c, void* stream, int type, const picasso_heads* q, const picasso_heads* k, const picasso_heads* v,
@@ -355,7 +348,7 @@ int picasso_attention_forward(picasso_ctx* c, void* stream, int type, const pica
             return PICASSO_ERR_INVALID_ARG;
     }
     const ForwardPlan p = forward_plan(a);
-    const size_t need = attention_forward_bytes(a);
+    const size_t need = attention_forward_bytes(a, p);
     if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16))) return PICASSO_ERR_WORKSPACE;
     if (Tq == 0) return PICASSO_OK;
     hipStream_t s = (hipStream_t)stream;
@@ -408,11 +401,11 @@ int picasso_attention_backward(picasso_ctx* c, void* stream, int type, const pic
                 return PICASSO_ERR_INVALID_ARG;
         }
     }
-    if (!d_workspace || workspace_bytes < attention_backward_bytes(a) || !aligned(d_workspace, 16)) return PICASSO_ERR_WORKSPACE;
+    const BackwardPlan p = backward_plan(a);
+    if (!d_workspace || workspace_bytes < attention_backward_bytes(a, p) || !aligned(d_workspace, 16)) return PICASSO_ERR_WORKSPACE;
     if (Tq == 0 && Tk == 0) return PICASSO_OK;
     hipStream_t s = (hipStream_t)stream;
     ON_DEVICE(c);
-    const BackwardPlan p = backward_plan(a);
     const attn::Offsets off{d_q_offsets, d_k_offsets, B, Tq, Tk};
     const attn::Group group = attn::heads_per_group(a.G());
     const attn::Scale sc{scale * attn::LOG2E, scale};

@@ -131,3 +131,13 @@ def test_clipping(lib, pk):
     four, kind = (ctypes.c_int64 * 1)(4), (ctypes.c_int32 * 1)(0)
     assert lib.picasso_gradient_norm(CTX, None, 1, one, four, kind, None, P[9], BIG) == pk.PICASSO_ERR_INVALID_ARG
     assert lib.picasso_gradient_norm(CTX, None, 1, one, four, kind, P[1], None, BIG) == pk.PICASSO_ERR_WORKSPACE
+
+
+@pytest.mark.parametrize("name", ["PK_RW", "PK_FS", "PK_KS", "PK_QS"])
+@pytest.mark.parametrize("value", ["0", "1", "7", "-1"])
+def test_the_environment_changes_no_plan(lib, monkeypatch, name, value):
+    sizes = [(t, b, tq, tk, 4, 2, 64) for t in (0, 1) for b, tq, tk in ((1, 1, 100000), (3, 24000, 24000), (16, 960, 960000), (2, 50, 60))]
+    ask = lambda: [lib.picasso_attention_workspace_bytes(*s, back) for s in sizes for back in (0, 1)]  # noqa: E731
+    before = ask()
+    monkeypatch.setenv(name, value)
+    assert ask() == before
