@@ -451,7 +451,11 @@ const at::Tensor* exactly(Args& a, const Where& w, const char* what, at::ScalarT
     }
     return t;
 }
-void* data(const at::Tensor* t) { return t ? t->data_ptr() : nullptr; }
+// A caller's tensor that the call has written: its version is raised, as by torch's own operations in place, so that a backward pass
+// that saved the old contents is refused rather than wrong.
+void written(const at::Tensor& t) {
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
 int as_i32(int64_t n, const char* what) {
     if (n > 0x7FFFFFFF) wrong(what, "less than 2^31 rows and columns");
     return (int)n;
@@ -483,6 +487,7 @@ PyObject* layer_norm_forward(Args& a) {
     checked(w.c, [&] {
         return picasso_layer_norm_forward(w.c, w.s, f.type, f.x.data_ptr(), f.N, f.C, F(gamma), F(beta), eps, y.data_ptr(), F(mean), F(rstd));
     });
+    if (out) written(*out);
     return pack({wrap(y), wrap(mean), wrap(rstd)});
 }
 
@@ -573,6 +578,7 @@ PyObject* attention_forward(Args& a) {
         return picasso_attention_forward(w.c, w.s, x.type, &x.q.h, &x.k.h, &x.v.h, I(x.qo), I(x.ko), x.B, x.Tq, x.Tk, x.Hq, x.Hkv, x.D, x.causal,
                                          x.scale, given.t == nullptr, &out.h, F(lse), bytes ? ws.data_ptr() : nullptr, bytes);
     });
+    if (given.t) written(*given.t);
     return pack({wrap(o), wrap(lse)});
 }
 
@@ -601,6 +607,8 @@ PyObject* attention_backward(Args& a) {
         return picasso_attention_backward(w.c, w.s, x.type, &gout.h, &x.q.h, &x.k.h, &x.v.h, &out.h, F(lse), I(x.qo), I(x.ko), x.B, x.Tq, x.Tk, x.Hq,
                                           x.Hkv, x.D, x.causal, x.scale, !given, &gq.h, &gk.h, &gv.h, ws.data_ptr(), bytes);
     });
+    if (given)
+        for (const at::Tensor* t : {&tq, &tk, &tv}) written(*t);
     return pack({wrap(tq), wrap(tk), wrap(tv)});
 }
 
@@ -665,6 +673,7 @@ PyObject* clip_gradients(Args& a) {
         return picasso_clip_gradients(w.c, w.s, g.n(), g.data.data(), g.sizes.data(), g.types.data(), max_norm, to.data(), F(norm), ws.data_ptr(),
                                       bytes);
     });
+    for (const at::Tensor& t : out ? out->held : g.held) written(t);
     return wrap(norm);
 }
 
