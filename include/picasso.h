@@ -497,7 +497,8 @@ int picasso_f2v_backward(picasso_ctx* ctx, void* stream, const float* d_gx, cons
  * never run at the same time); too small or NULL: PICASSO_ERR_WORKSPACE.
  * Features are of one of the types below, all arithmetic is binary32 or more, a result is
  * rounded once; parameters, their gradients and statistics are float32.  Sums are made in a
- * fixed order, without atomics.  Outputs do not overlap inputs, unless said so; where that is seen the call is refused.
+ * fixed order, without atomics.  What a call writes (outputs, statistics, the workspace) overlaps nothing else that it reads
+ * or writes, unless said so.  Where it does the call is refused (not seen: two arrays of heads of different strides that interleave).
  * ------------------------------------------------------------------------- */
 enum picasso_type {
     PICASSO_F32 = 0,  /* binary32 */

@@ -7,6 +7,7 @@
 #include <stdio.h>
 
 #include <algorithm>
+#include <initializer_list>
 #include <vector>
 
 #include "../../include/picasso.h"
@@ -52,10 +53,69 @@ size_t size_of(int type) { return type == PICASSO_F32 ? 4 : 2; }
 size_t up(size_t x) { return (x + 255) / 256 * 256; }
 bool aligned(const void* p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
-// Whether two ranges of memory have a byte in common.
-bool meet(const void* a, size_t na, const void* b, size_t nb) {
-    const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-    return a && b && na && nb && x < y + nb && y < x + na;
+// Memory that a call reads or writes, in bytes: `rows` times `heads` stretches of `width`, `row` and `head` apart.
+struct Span {
+    uintptr_t p;
+    int64_t rows, row, heads, head, width;
+    bool out;
+    Span(const void* p_, int64_t rows_, int64_t row_, int64_t heads_, int64_t head_, int64_t width_, bool out_)
+        : p((uintptr_t)p_), rows(rows_), row(row_), heads(heads_), head(head_), width(p_ ? width_ : 0), out(out_) {
+        if (row == 0) rows = std::min<int64_t>(rows, 1);  // (broadcast)
+        if (head == 0) heads = std::min<int64_t>(heads, 1);
+        // stretches without a gap are one
+        if (heads > 1 && head == width) width *= heads, heads = 1;
+        if (rows > 1 && row == width) width *= rows, rows = 1;
+        if (heads > 1 && head == width) width *= heads, heads = 1;
+    }
+    bool empty() const { return rows <= 0 || heads <= 0 || width <= 0; }
+    int64_t extent() const { return empty() ? 0 : (rows - 1) * row + (heads - 1) * head + width; }
+};
+Span whole(const void* p, size_t bytes, bool out) { return Span(p, 1, 0, 1, 0, (int64_t)bytes, out); }
+
+int64_t floor_div(int64_t x, int64_t y) { return x / y - (x % y < 0); }
+
+// Whether a multiple of `row` by something from lo to hi puts x within (-below, above).
+bool hits(int64_t x, int64_t row, int64_t lo, int64_t hi, int64_t below, int64_t above) {
+    if (row == 0) return -below < x && x < above;
+    return std::max(lo, floor_div(x - above, row) + 1) <= std::min(hi, floor_div(x + below - 1, row));
+}
+
+// Whether two spans have a byte in common.  Of arrays whose strides differ along an axis that both have it is not known: false.
+bool meet(const Span& a, const Span& b) {
+    if (a.empty() || b.empty() || a.p >= b.p + (uintptr_t)b.extent() || b.p >= a.p + (uintptr_t)a.extent()) return false;
+    if ((a.rows > 1 && b.rows > 1 && a.row != b.row) || (a.heads > 1 && b.heads > 1 && a.head != b.head)) return false;
+    const int64_t row = a.rows > 1 ? a.row : b.rows > 1 ? b.row : 0, head = a.heads > 1 ? a.head : b.heads > 1 ? b.head : 0, apart = (int64_t)(b.p - a.p);
+    // parts of one projection, side by side in each row (what is passed as a rule)
+    const int64_t wa = (a.heads - 1) * head + a.width, wb = (b.heads - 1) * head + b.width;
+    if (row > 0) {
+        const int64_t r = apart - floor_div(apart, row) * row;
+        if (r >= wa && r + wb <= row) return false;
+    }
+    for (int64_t h = 1 - b.heads; h < a.heads; ++h)
+        if (hits(apart - h * head, row, 1 - b.rows, a.rows - 1, b.width, a.width)) return true;
+    return false;
+}
+
+// Whether two stretches of one array lie over each other.
+bool folded(const Span& a) {
+    if (a.empty()) return false;
+    if (a.rows > 1 && a.row < a.width) return true;
+    if (a.heads > 1 && a.head < a.width) return true;
+    if (a.rows == 1 || a.heads == 1 || (a.heads - 1) * a.head + a.width <= a.row || (a.rows - 1) * a.row + a.width <= a.head) return false;
+    for (int64_t h = 1; h < a.heads; ++h)
+        if (hits(-h * a.head, a.row, 1 - a.rows, a.rows - 1, a.width, a.width)) return true;
+    return false;
+}
+
+// What is written lies over nothing else that the call reads or writes.
+bool apart(std::initializer_list<Span> all) {
+    for (const Span* a = all.begin(); a != all.end(); ++a) {
+        if (!a->out) continue;
+        if (folded(*a)) return false;
+        for (const Span* b = all.begin(); b != all.end(); ++b)
+            if (a != b && (!b->out || a < b) && meet(*a, *b)) return false;
+    }
+    return true;
 }
 
 // CALL(T) for the features' type
@@ -204,14 +264,16 @@ size_t attention_backward_bytes(const Attention& a, const BackwardPlan& p) {
 }
 
 // An array of heads as the kernels take it: 16-byte aligned rows and heads.
-bool valid_heads(const picasso_heads* h, const Attention& a, int rows, bool output) {
+bool valid_heads(const picasso_heads* h, const Attention& a, int rows, int heads, bool output) {
     if (!h || (rows > 0 && !h->data)) return false;
     const long long each = (long long)(16 / size_of(a.type)), least = output ? a.D : 0;
     return aligned(h->data, 16) && h->row_stride >= least && h->head_stride >= least && h->row_stride % each == 0 && h->head_stride % each == 0 &&
-           h->row_stride <= (1ll << 40) && h->head_stride <= (1ll << 40);
+           h->row_stride <= (1ll << 40) && h->head_stride <= (1ll << 40) &&
+           (__int128)rows * h->row_stride + (__int128)heads * h->head_stride <= ((__int128)1 << 48);  // (no memory is larger)
 }
-size_t extent(const picasso_heads* h, const Attention& a, int rows, int heads) {
-    return rows ? (size_t)((rows - 1) * h->row_stride + (heads - 1) * h->head_stride + a.D) * size_of(a.type) : 0;
+Span span(const picasso_heads* h, const Attention& a, int rows, int heads, bool out) {
+    const int64_t size = (int64_t)size_of(a.type);
+    return Span(h->data, rows, h->row_stride * size, heads, h->head_stride * size, a.D * size, out);
 }
 template <typename T>
 attn::Heads<T> heads(const picasso_heads* h) {
@@ -225,10 +287,6 @@ attn::Heads<T> heads(const picasso_heads* h) {
         else if ((D) <= 64) { CALL(T, 64); }       \
         else { CALL(T, 128); }                     \
     } while (0)
-
-// (outputs whose rows and heads interleave, as the parts of one projection do, may share a range of memory: only inputs are held
-// apart from outputs, and only where an output is a whole range by itself)
-bool dense(const picasso_heads* h, const Attention& a, int heads) { return h->head_stride == a.D && h->row_stride == (int64_t)heads * a.D; }
 
 // ---- gradients --------------------------------------------------------------------------------------
 
@@ -265,6 +323,40 @@ bool valid_gradients(int n, const void* const* in, const int64_t* sizes, const i
     return true;
 }
 
+// What is written lies over nothing else: an output may be its own gradient, and nothing more (a tensor that is listed twice would be
+// scaled twice, or once and a half); the norm and the workspace are no tensor's memory.  out: null, where tensors are only read.
+int tensors_apart(int n, const void* const* in, void* const* out, const int64_t* sizes, const int32_t* types, const float* norm,
+                  const void* ws, size_t ws_bytes) {
+    struct Range {
+        uintptr_t from, to;
+        bool out;
+    };
+    std::vector<Range> r;
+    try {
+        r.reserve(2 * (size_t)n + 2);
+    } catch (...) {
+        return PICASSO_ERR_WORKSPACE;
+    }
+    const auto add = [&](const void* p, uintptr_t bytes, bool written) {
+        if (p && bytes) r.push_back(Range{(uintptr_t)p, (uintptr_t)p + bytes, written});
+    };
+    add(norm, sizeof(float), true);
+    add(ws, ws_bytes, true);
+    for (int k = 0; k < n; ++k) {
+        const uintptr_t bytes = (uintptr_t)sizes[k] * size_of(types[k]);
+        if (out) add(out[k], bytes, true);
+        if (!out || out[k] != in[k]) add(in[k], bytes, false);
+    }
+    std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+    uintptr_t end_out = 0, end_any = 0;  // of those that start before
+    for (const Range& x : r) {
+        if (x.from < (x.out ? end_any : end_out)) return PICASSO_ERR_INVALID_ARG;
+        end_any = std::max(end_any, x.to);
+        if (x.out) end_out = std::max(end_out, x.to);
+    }
+    return PICASSO_OK;
+}
+
 // Partials of all tensors' squares in ws; how many.
 int queue_squares(hipStream_t s, int n, const void* const* in, const int64_t* sizes, const int32_t* types, double* ws) {
     int partials = 0;
@@ -283,8 +375,11 @@ int picasso_layer_norm_forward(picasso_ctx* c, void* stream, int type, const voi
                                const float* d_beta, float eps, void* d_y, float* d_mean, float* d_rstd) {
     if (!c || !known_type(type) || N < 0 || C < 1 || !(eps >= 0.0f) || !std::isfinite(eps) || (N > 0 && (!d_x || !d_y)))
         return PICASSO_ERR_INVALID_ARG;
-    const size_t bytes = (size_t)N * C * size_of(type);
-    if (!aligned(d_x, size_of(type)) || !aligned(d_y, size_of(type)) || meet(d_x, bytes, d_y, bytes)) return PICASSO_ERR_INVALID_ARG;
+    const size_t bytes = (size_t)N * C * size_of(type), stats = (size_t)N * 4, params = (size_t)C * 4;
+    if (!aligned(d_x, size_of(type)) || !aligned(d_y, size_of(type)) ||
+        !apart({whole(d_x, bytes, false), whole(d_gamma, params, false), whole(d_beta, params, false), whole(d_y, bytes, true),
+                whole(d_mean, stats, true), whole(d_rstd, stats, true)}))
+        return PICASSO_ERR_INVALID_ARG;
     if (N == 0) return PICASSO_OK;
     hipStream_t s = (hipStream_t)stream;
     ON_DEVICE(c);
@@ -305,12 +400,15 @@ int picasso_layer_norm_backward(picasso_ctx* c, void* stream, int type, const vo
                                 float* d_gbeta, void* d_workspace, size_t workspace_bytes) {
     if (!c || !known_type(type) || N < 0 || C < 1 || (N > 0 && (!d_gy || !d_x || !d_mean || !d_rstd)) || (!d_gx && !d_ggamma && !d_gbeta))
         return PICASSO_ERR_INVALID_ARG;
-    const size_t bytes = (size_t)N * C * size_of(type);
-    if (!aligned(d_gy, size_of(type)) || !aligned(d_x, size_of(type)) || !aligned(d_gx, size_of(type)) || meet(d_x, bytes, d_gx, bytes) ||
-        meet(d_gy, bytes, d_gx, bytes))
-        return PICASSO_ERR_INVALID_ARG;
+    if (!aligned(d_gy, size_of(type)) || !aligned(d_x, size_of(type)) || !aligned(d_gx, size_of(type))) return PICASSO_ERR_INVALID_ARG;
     const bool sums = d_ggamma || d_gbeta;
-    if (sums && (!d_workspace || workspace_bytes < picasso_layer_norm_workspace_bytes(type, N, C))) return PICASSO_ERR_WORKSPACE;
+    const size_t bytes = (size_t)N * C * size_of(type), stats = (size_t)N * 4, params = (size_t)C * 4,
+                 need = sums ? picasso_layer_norm_workspace_bytes(type, N, C) : 0;
+    if (!apart({whole(d_gy, bytes, false), whole(d_x, bytes, false), whole(d_gamma, params, false), whole(d_mean, stats, false),
+                whole(d_rstd, stats, false), whole(d_gx, bytes, true), whole(d_ggamma, params, true), whole(d_gbeta, params, true),
+                whole(d_workspace, std::min(need, workspace_bytes), true)}))
+        return PICASSO_ERR_INVALID_ARG;
+    if (sums && (!d_workspace || workspace_bytes < need)) return PICASSO_ERR_WORKSPACE;
     if (N == 0 && !sums) return PICASSO_OK;
     hipStream_t s = (hipStream_t)stream;
     ON_DEVICE(c);
@@ -338,17 +436,16 @@ int picasso_attention_forward(picasso_ctx* c, void* stream, int type, const pica
                               int32_t Hkv, int32_t D, int causal, float scale, int clear_outside, const picasso_heads* out, float* d_lse,
                               void* d_workspace, size_t workspace_bytes) {
     const Attention a{type, B, Tq, Tk, Hq, Hkv, D};
-    if (!c || !valid(a) || !valid_heads(q, a, Tq, false) || !valid_heads(k, a, Tk, false) || !valid_heads(v, a, Tk, false) ||
-        !valid_heads(out, a, Tq, true) || !d_q_offsets || !d_k_offsets || !(scale > 0.0f) || !std::isfinite(scale))
+    if (!c || !valid(a) || !valid_heads(q, a, Tq, Hq, false) || !valid_heads(k, a, Tk, Hkv, false) || !valid_heads(v, a, Tk, Hkv, false) ||
+        !valid_heads(out, a, Tq, Hq, true) || !d_q_offsets || !d_k_offsets || !(scale > 0.0f) || !std::isfinite(scale))
         return PICASSO_ERR_INVALID_ARG;
-    if (dense(out, a, Hq)) {
-        const size_t n = extent(out, a, Tq, Hq);
-        if (meet(out->data, n, q->data, extent(q, a, Tq, Hq)) || meet(out->data, n, k->data, extent(k, a, Tk, Hkv)) ||
-            meet(out->data, n, v->data, extent(v, a, Tk, Hkv)))
-            return PICASSO_ERR_INVALID_ARG;
-    }
     const ForwardPlan p = forward_plan(a);
     const size_t need = attention_forward_bytes(a, p);
+    const size_t offsets = ((size_t)B + 1) * 4;
+    if (!apart({span(q, a, Tq, Hq, false), span(k, a, Tk, Hkv, false), span(v, a, Tk, Hkv, false), whole(d_q_offsets, offsets, false),
+                whole(d_k_offsets, offsets, false), span(out, a, Tq, Hq, true), whole(d_lse, (size_t)Tq * Hq * 4, true),
+                whole(d_workspace, std::min(need, workspace_bytes), true)}))
+        return PICASSO_ERR_INVALID_ARG;
     if (need && (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16))) return PICASSO_ERR_WORKSPACE;
     if (Tq == 0) return PICASSO_OK;
     hipStream_t s = (hipStream_t)stream;
@@ -385,24 +482,18 @@ int picasso_attention_backward(picasso_ctx* c, void* stream, int type, const pic
                                int32_t Hkv, int32_t D, int causal, float scale, int clear_outside, const picasso_heads* gq,
                                const picasso_heads* gk, const picasso_heads* gv, void* d_workspace, size_t workspace_bytes) {
     const Attention a{type, B, Tq, Tk, Hq, Hkv, D};
-    if (!c || !valid(a) || !valid_heads(gout, a, Tq, false) || !valid_heads(q, a, Tq, false) || !valid_heads(k, a, Tk, false) ||
-        !valid_heads(v, a, Tk, false) || !valid_heads(out, a, Tq, false) || !valid_heads(gq, a, Tq, true) || !valid_heads(gk, a, Tk, true) ||
-        !valid_heads(gv, a, Tk, true) || (Tq > 0 && !d_lse) || !d_q_offsets || !d_k_offsets || !(scale > 0.0f) || !std::isfinite(scale))
+    if (!c || !valid(a) || !valid_heads(gout, a, Tq, Hq, false) || !valid_heads(q, a, Tq, Hq, false) || !valid_heads(k, a, Tk, Hkv, false) ||
+        !valid_heads(v, a, Tk, Hkv, false) || !valid_heads(out, a, Tq, Hq, false) || !valid_heads(gq, a, Tq, Hq, true) ||
+        !valid_heads(gk, a, Tk, Hkv, true) || !valid_heads(gv, a, Tk, Hkv, true) || (Tq > 0 && !d_lse) || !d_q_offsets || !d_k_offsets || !(scale > 0.0f) || !std::isfinite(scale))
         return PICASSO_ERR_INVALID_ARG;
-    const picasso_heads* const outputs[3] = {gq, gk, gv};
-    const picasso_heads* const inputs[5] = {gout, q, k, v, out};
-    for (int i = 0; i < 3; ++i) {
-        const int rows = i ? Tk : Tq, heads_ = i ? Hkv : Hq;
-        if (!dense(outputs[i], a, heads_)) continue;
-        for (int j = 0; j < 5; ++j) {
-            const bool keys = j == 2 || j == 3;
-            if (meet(outputs[i]->data, extent(outputs[i], a, rows, heads_), inputs[j]->data,
-                     extent(inputs[j], a, keys ? Tk : Tq, keys ? Hkv : Hq)))
-                return PICASSO_ERR_INVALID_ARG;
-        }
-    }
     const BackwardPlan p = backward_plan(a);
-    if (!d_workspace || workspace_bytes < attention_backward_bytes(a, p) || !aligned(d_workspace, 16)) return PICASSO_ERR_WORKSPACE;
+    const size_t need = attention_backward_bytes(a, p), offsets = ((size_t)B + 1) * 4;
+    if (!apart({span(gout, a, Tq, Hq, false), span(q, a, Tq, Hq, false), span(k, a, Tk, Hkv, false), span(v, a, Tk, Hkv, false),
+                span(out, a, Tq, Hq, false), whole(d_lse, (size_t)Tq * Hq * 4, false), whole(d_q_offsets, offsets, false),
+                whole(d_k_offsets, offsets, false), span(gq, a, Tq, Hq, true), span(gk, a, Tk, Hkv, true), span(gv, a, Tk, Hkv, true),
+                whole(d_workspace, std::min(need, workspace_bytes), true)}))
+        return PICASSO_ERR_INVALID_ARG;
+    if (!d_workspace || workspace_bytes < need || !aligned(d_workspace, 16)) return PICASSO_ERR_WORKSPACE;
     if (Tq == 0 && Tk == 0) return PICASSO_OK;
     hipStream_t s = (hipStream_t)stream;
     ON_DEVICE(c);
@@ -460,7 +551,9 @@ size_t picasso_gradients_workspace_bytes(int32_t n, const int64_t* h_sizes) {
 int picasso_gradient_norm(picasso_ctx* c, void* stream, int32_t n, const void* const* h_grads, const int64_t* h_sizes,
                           const int32_t* h_types, float* d_norm, void* d_workspace, size_t workspace_bytes) {
     if (!c || !valid_gradients(n, h_grads, h_sizes, h_types) || !d_norm) return PICASSO_ERR_INVALID_ARG;
-    if (!d_workspace || !aligned(d_workspace, 8) || workspace_bytes < picasso_gradients_workspace_bytes(n, h_sizes)) return PICASSO_ERR_WORKSPACE;
+    const size_t need = picasso_gradients_workspace_bytes(n, h_sizes);
+    if (const int rc = tensors_apart(n, h_grads, nullptr, h_sizes, h_types, d_norm, d_workspace, std::min(need, workspace_bytes))) return rc;
+    if (!d_workspace || !aligned(d_workspace, 8) || workspace_bytes < need) return PICASSO_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;
     ON_DEVICE(c);
     double* ws = (double*)d_workspace;
@@ -476,33 +569,9 @@ int picasso_clip_gradients(picasso_ctx* c, void* stream, int32_t n, const void* 
     if (!c || !valid_gradients(n, h_grads, h_sizes, h_types) || !(max_norm >= 0.0) || (n > 0 && !h_out)) return PICASSO_ERR_INVALID_ARG;
     for (int k = 0; k < n; ++k)
         if ((h_sizes[k] > 0 && !h_out[k]) || !aligned(h_out[k], size_of(h_types[k]))) return PICASSO_ERR_INVALID_ARG;
-    if (!d_workspace || !aligned(d_workspace, 8) || workspace_bytes < picasso_gradients_workspace_bytes(n, h_sizes)) return PICASSO_ERR_WORKSPACE;
-    // an output may be its own gradient, and nothing else: a tensor that is listed twice would be scaled twice, or once and a half
-    {
-        struct Range {
-            uintptr_t from, to;
-            bool out;
-        };
-        std::vector<Range> r;
-        try {
-            r.reserve(2 * (size_t)n);
-            for (int k = 0; k < n; ++k) {
-                const uintptr_t bytes = (uintptr_t)h_sizes[k] * size_of(h_types[k]);
-                if (!bytes) continue;
-                r.push_back(Range{(uintptr_t)h_out[k], (uintptr_t)h_out[k] + bytes, true});
-                if (h_out[k] != h_grads[k]) r.push_back(Range{(uintptr_t)h_grads[k], (uintptr_t)h_grads[k] + bytes, false});
-            }
-        } catch (...) {
-            return PICASSO_ERR_WORKSPACE;
-        }
-        std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
-        uintptr_t end_out = 0, end_any = 0;  // of those that start before
-        for (const Range& x : r) {
-            if (x.from < (x.out ? end_any : end_out)) return PICASSO_ERR_INVALID_ARG;
-            end_any = std::max(end_any, x.to);
-            if (x.out) end_out = std::max(end_out, x.to);
-        }
-    }
+    const size_t need = picasso_gradients_workspace_bytes(n, h_sizes);
+    if (const int rc = tensors_apart(n, h_grads, h_out, h_sizes, h_types, d_norm, d_workspace, std::min(need, workspace_bytes))) return rc;
+    if (!d_workspace || !aligned(d_workspace, 8) || workspace_bytes < need) return PICASSO_ERR_WORKSPACE;
     hipStream_t s = (hipStream_t)stream;
     ON_DEVICE(c);
     double* ws = (double*)d_workspace;

@@ -141,3 +141,131 @@ def test_the_environment_changes_no_plan(lib, monkeypatch, name, value):
     before = ask()
     monkeypatch.setenv(name, value)
     assert ask() == before
+
+
+# ---- outputs over other arrays of a call.  (No call here is accepted: where nothing overlaps the workspace is missing.)
+
+
+def backward(lib, pk, arrays, Tq, Tk, Hq, Hkv, D, lse=0x40000000, ws=None):
+    """arrays: {name: (address, row stride, head stride)}, the others far from everything; float32."""
+    names = ["gout", "q", "k", "v", "out", "gq", "gk", "gv"]
+    far = {n: (0x100000000 * (i + 1), 1 << 12, 1 << 6) for i, n in enumerate(names)}
+    h = [ctypes.byref(pk.picasso_heads(*{**far, **arrays}[n])) for n in names]
+    return lib.picasso_attention_backward(CTX, None, 0, *h[:5], ctypes.c_void_p(lse), ctypes.c_void_p(0x50000000), ctypes.c_void_p(0x60000000), 1, Tq, Tk, Hq,
+                                          Hkv, D, 0, 1.0, 1, *h[5:], ctypes.c_void_p(ws), BIG if ws else 0)
+
+
+def test_parts_of_one_array(lib, pk):
+    INVALID, WS = pk.PICASSO_ERR_INVALID_ARG, pk.PICASSO_ERR_WORKSPACE
+    T, H, D = 100, 4, 32
+    at = lambda part, base=0x10000000: (base + 4 * part * H * D, 3 * H * D, D)  # noqa: E731  [T, 3, H, D]
+    qkv = dict(q=at(0), k=at(1), v=at(2))
+    grads = dict(gq=at(0, 0x20000000), gk=at(1, 0x20000000), gv=at(2, 0x20000000))
+    assert backward(lib, pk, {**qkv, **grads}, T, T, H, H, D) == WS
+    for name in ("q", "k", "v"):                       # a gradient in place of an input that other workgroups still read
+        for g in ("gq", "gk", "gv"):
+            assert backward(lib, pk, {**qkv, **grads, g: qkv[name]}, T, T, H, H, D) == INVALID, (name, g)
+    assert backward(lib, pk, {**qkv, **grads, "gk": grads["gv"]}, T, T, H, H, D) == INVALID
+    assert backward(lib, pk, {**qkv, **grads, "gk": grads["gq"]}, T, T, H, H, D) == INVALID
+    per_head = lambda part, base=0x10000000: (base + 4 * part * D, 3 * H * D, 3 * D)  # noqa: E731  [T, H, 3, D]
+    both = dict(q=per_head(0), k=per_head(1), v=per_head(2), gq=per_head(0, 0x20000000), gk=per_head(1, 0x20000000), gv=per_head(2, 0x20000000))
+    assert backward(lib, pk, both, T, T, H, H, D) == WS
+    assert backward(lib, pk, {**both, "gv": both["gq"]}, T, T, H, H, D) == INVALID
+    outermost = lambda part, base=0x10000000: (base + 4 * part * H * T * D, D, T * D)  # noqa: E731  [3, H, T, D]
+    both = dict(q=outermost(0), k=outermost(1), v=outermost(2), gq=outermost(0, 0x20000000), gk=outermost(1, 0x20000000), gv=outermost(2, 0x20000000))
+    assert backward(lib, pk, both, T, T, H, H, D) == WS
+    assert backward(lib, pk, {**both, "gk": both["v"]}, T, T, H, H, D) == INVALID
+    # rows and heads of one output over one another
+    assert backward(lib, pk, dict(gq=(0x20000000, D, D)), T, T, H, H, D) == INVALID
+    assert backward(lib, pk, dict(gq=(0x20000000, 3 * D, 2 * D)), T, T, H, H, D) == INVALID
+    assert backward(lib, pk, dict(gq=(0x20000000, 2 * D, 1 << 20)), T, T, H, H, D) == WS
+    # the statistics and the workspace
+    assert backward(lib, pk, {**qkv, **grads}, T, T, H, H, D, lse=0x20000000 + 64) == INVALID
+    assert backward(lib, pk, {**qkv, **grads}, T, T, H, H, D, ws=0x10000000) == INVALID
+    assert backward(lib, pk, {**qkv, **grads}, T, T, H, H, D, ws=0x20000000) == INVALID
+    assert backward(lib, pk, {**qkv, **grads}, T, T, H, H, D, ws=0x50000000 - 1024) == INVALID
+
+
+def test_overlaps_against_a_count_of_bytes(lib, pk):
+    """Two arrays of heads at random places: refused exactly where a byte is in both, if their strides are alike; where they differ, never
+    without one."""
+    import random
+    rng = random.Random(7)
+    seen = {True: 0, False: 0}
+    for _ in range(4000):
+        D = rng.choice((8, 16))
+        T, S, H, G = rng.randint(1, 6), rng.randint(1, 6), rng.randint(1, 4), rng.randint(1, 2)
+        G = G if H % G == 0 else 1
+        strides = [(rng.randint(D // 4, 60) * 4, rng.randint(D // 4, 60) * 4) for _ in range(2)]
+        alike = rng.random() < 0.7
+        (r0, h0), (r1, h1) = strides[0], strides[0] if alike else strides[1]
+        base, other = 0x10000000, 0x10000000 + 16 * rng.randint(-120, 120)
+        cells = lambda p, n, r, m, h: [p // 4 + i * r + j * h + d for i in range(n) for j in range(m) for d in range(D)]  # noqa: E731
+        # gk [S, G, D] against q [T, H, D]
+        a, b = cells(base, S, r0, G, h0), cells(other, T, r1, H, h1)
+        over = len(set(a)) < len(a) or bool(set(a) & set(b))
+        st = backward(lib, pk, dict(gk=(base, r0, h0), q=(other, r1, h1)), T, S, H, G, D)
+        assert st in (pk.PICASSO_ERR_INVALID_ARG, pk.PICASSO_ERR_WORKSPACE)
+        refused = st == pk.PICASSO_ERR_INVALID_ARG
+        if alike:
+            assert refused == over, (D, T, S, H, G, r0, h0, other - base)
+        else:
+            assert not refused or over, (D, T, S, H, G, strides, other - base)
+        seen[refused] += 1
+    assert min(seen.values()) > 500
+
+
+def test_forward_overlaps(lib, pk):
+    INVALID, WS = pk.PICASSO_ERR_INVALID_ARG, pk.PICASSO_ERR_WORKSPACE
+    T, n = 8, 100000                                    # few queries over many keys: split, so a workspace is needed
+
+    def call(out, lse=0x70000000, ws=None, **change):
+        a = dict(q=(0x10000000, 128, 32), k=(0x20000000, 192, 32), v=(0x20000000 + 256, 192, 32))
+        a.update(change)
+        h = {k: ctypes.byref(pk.picasso_heads(*x)) for k, x in dict(a, out=out).items()}
+        return lib.picasso_attention_forward(CTX, None, 0, h["q"], h["k"], h["v"], ctypes.c_void_p(0x50000000), ctypes.c_void_p(0x60000000), 1, T, n, 4, 2, 32, 0,
+                                             1.0, 1, h["out"], ctypes.c_void_p(lse), ctypes.c_void_p(ws), BIG if ws else 0)
+    assert call((0x40000000, 128, 32)) == WS
+    assert call((0x20000000 + 512, 192, 16)) == INVALID             # (heads over one another)
+    assert call((0x20000000 + 256, 192, 32)) == INVALID             # in place of v, a part of a projection's output
+    assert call((0x10000000, 128, 32)) == INVALID
+    assert call((0x40000000, 128, 32), lse=0x40000040) == INVALID
+    assert call((0x40000000, 128, 32), lse=0x20000000) == INVALID
+    assert call((0x40000000, 128, 32), ws=0x40000000 - 4096) == INVALID
+    assert call((0x40000000, 128, 32), ws=0x20001000) == INVALID
+    assert call((0x40000000, 1 << 40, 1 << 40), T) == INVALID       # (an array of 2^43 values and more)
+
+
+def test_layer_norm_overlaps(lib, pk):
+    x, y, a, b, c, d, e, ws = (0x10000000 * (k + 1) for k in range(8))
+    V = ctypes.c_void_p
+
+    def forward(gamma=a, beta=b, out=y, mean=c, rstd=d):
+        return lib.picasso_layer_norm_forward(CTX, None, 0, V(x), 100, 64, V(gamma), V(beta), 1e-5, V(out), V(mean), V(rstd))
+    for change in (dict(out=a + 16), dict(out=b), dict(mean=y + 400), dict(rstd=c), dict(mean=x), dict(rstd=a), dict(out=x + 4)):
+        assert forward(**change) == pk.PICASSO_ERR_INVALID_ARG, change
+    need = lib.picasso_layer_norm_workspace_bytes(0, 100, 64)
+
+    def backward(gx=c, gg=d, gb=e, w=ws, n=need):
+        return lib.picasso_layer_norm_backward(CTX, None, 0, V(x), V(y), 100, 64, V(a), V(b), V(b + 1024), V(gx), V(gg), V(gb), V(w), n)
+    assert backward(n=need - 1) == pk.PICASSO_ERR_WORKSPACE
+    for change in (dict(gx=x), dict(gx=y), dict(gx=a), dict(gg=e), dict(gg=a), dict(gb=b), dict(gg=c + 64), dict(w=c), dict(w=x + 1024), dict(w=b), dict(gb=ws)):
+        assert backward(**change) == pk.PICASSO_ERR_INVALID_ARG, change
+
+
+def test_clipping_overlaps(lib, pk):
+    x, y, norm, ws = 0x10000000, 0x20000000, 0x30000000, 0x40000000
+    two, sizes, types, V = (ctypes.c_void_p * 2)(x, y), (ctypes.c_int64 * 2)(1000, 2000), (ctypes.c_int32 * 2)(0, 1), ctypes.c_void_p
+
+    def clip(norm=norm, ws=ws, out=two, n=BIG):
+        return lib.picasso_clip_gradients(CTX, None, 2, two, sizes, types, 1.0, out, V(norm), V(ws), n)
+
+    def plain(norm=norm, ws=ws, n=BIG):
+        return lib.picasso_gradient_norm(CTX, None, 2, two, sizes, types, V(norm), V(ws), n)
+    assert clip(n=0) == pk.PICASSO_ERR_WORKSPACE and plain(n=0) == pk.PICASSO_ERR_WORKSPACE
+    for f in (clip, plain):
+        for change in (dict(norm=x + 40), dict(norm=y + 3996), dict(ws=x + 8), dict(ws=y), dict(norm=ws)):
+            assert f(**change) == pk.PICASSO_ERR_INVALID_ARG, change
+    to = (ctypes.c_void_p * 2)(0x50000000, 0x60000000)
+    for change in (dict(norm=x), dict(norm=0x50000000 + 400), dict(ws=0x60000000)):
+        assert clip(out=to, **change) == pk.PICASSO_ERR_INVALID_ARG, change

@@ -364,3 +364,32 @@ def test_float16_gradients_of_far_sizes_side_by_side(ctx):
     held(gk, (value, bar + scale * 2.0 ** -38 * (ds.abs().amax(0)[:, None] * Q.abs().sum(0))[:, None] + 2.0 ** -25), "gk")
     value, bar = want["gq"]
     held(gq, (value, bar + scale * 2.0 ** -38 * (ds.abs().amax(1)[:, None] * K.abs().sum(0))[:, None] + 2.0 ** -25), "gq")
+
+
+def test_outputs_as_parts_of_the_inputs_array(ctx):
+    """Every way that parts of one array lie beside each other is taken as an output; what lies over an input is refused and left as it was."""
+    import paper_2103_15076_amd as pk
+    T, H, D = 150, 2, 32
+    o = offsets([90, 60])
+    for shape, cut in (((T, 4, H, D), lambda a, i: a[:, i]), ((T, H, 4, D), lambda a, i: a[:, :, i]), ((4, H, T, D), lambda a, i: a[i].transpose(0, 1)),
+                       ((H, T, 4, D), lambda a, i: a[:, :, i].transpose(0, 1))):
+        a = torch.randn(shape, device="cuda")
+        q, k, v, to = (cut(a, i) for i in range(4))
+        before = a.clone()
+        want, lse = ctx.picasso_attention_forward(q.contiguous(), k.contiguous(), v.contiguous(), o)
+        ctx.picasso_attention_forward(q, k, v, o, out=to)
+        assert torch.equal(to, want) and all(torch.equal(cut(a, i), cut(before, i)) for i in range(3))
+        g = torch.zeros_like(a)
+        go = torch.randn(T, H, D, device="cuda")
+        ctx.picasso_attention_backward(go, q, k, v, to, lse, o, grads=tuple(cut(g, i) for i in range(3)))
+        plain = ctx.picasso_attention_backward(go, q.contiguous(), k.contiguous(), v.contiguous(), want, lse, o)
+        assert all(torch.equal(cut(g, i), plain[i]) for i in range(3)) and (cut(g, 3) == 0).all()
+        for over in (q, k, v):
+            with pytest.raises(pk.PicassoError) as e:
+                ctx.picasso_attention_forward(q, k, v, o, out=over)
+            assert e.value.status == pk.PICASSO_ERR_INVALID_ARG
+            with pytest.raises(pk.PicassoError):
+                ctx.picasso_attention_backward(go, q, k, v, to, lse, o, grads=(cut(g, 0), cut(g, 1), over))
+        with pytest.raises(pk.PicassoError):
+            ctx.picasso_attention_backward(go, q, k, v, to, lse, o, grads=(cut(g, 0), cut(g, 1), cut(g, 1)))
+        assert all(torch.equal(cut(a, i), cut(before, i)) for i in range(3))
