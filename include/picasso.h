@@ -541,7 +541,7 @@ typedef struct picasso_heads {
  * Rows of no sequence (in front of the first, behind the last) are left as they were, or, with clear_outside, get what
  * a query without keys gets.  A causal call's non-finite keys and values may reach queries in front of them; those of
  * another sequence or of rows of none never do.  Hq a multiple of Hkv (at most 65535), D a multiple of 8 up to 128,
- * Tq * Hq / Hkv and Tk up to 2^30, B up to 2^24, scale finite and positive. */
+ * Tq * Hq / Hkv and Tk up to 2^30, B and a 128th of either of them together up to 2^24 - 3, scale finite and positive. */
 size_t picasso_attention_workspace_bytes(int type, int32_t B, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv, int32_t D,
                                          int backward);
 int picasso_attention_forward(picasso_ctx* ctx, void* stream, int type, const picasso_heads* q, const picasso_heads* k,

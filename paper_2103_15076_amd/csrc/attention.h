@@ -503,32 +503,33 @@ template <typename T>
 __global__ __launch_bounds__(BLOCK) void join_kernel(const float* __restrict__ part_out, const float* __restrict__ part_lse, int splits,
                                                      Offsets off, int Hq, int D, int clear, Heads<T> out, float* __restrict__ lse) {
     const int packs = D / 4;
-    const long long i = (long long)blockIdx.x * BLOCK + threadIdx.x, rows = (long long)off.Tq * Hq;
-    const long long row = i / packs;
-    if (row >= rows) return;
-    const int d = (int)(i % packs) * 4, head = (int)(row / off.Tq), t = (int)(row % off.Tq);
-    if (!clear && (t < clipped(off.q[0], off.Tq) || t >= clipped(off.q[off.B], off.Tq))) return;  // (rows of no sequence stay)
-    float m = -INFINITY;
-    for (int s = 0; s < splits; ++s) m = fmaxf(m, part_lse[(size_t)s * rows + row]);
-    const float base = m == -INFINITY ? 0.0f : m;
-    float l = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < splits; ++s) {
-        const float w = __builtin_amdgcn_exp2f(part_lse[(size_t)s * rows + row] - base);
-        const float4 x = *reinterpret_cast<const float4*>(part_out + ((size_t)s * rows + row) * D + d);
-        l += w;
-        acc[0] = fmaf(w, x.x, acc[0]);
-        acc[1] = fmaf(w, x.y, acc[1]);
-        acc[2] = fmaf(w, x.z, acc[2]);
-        acc[3] = fmaf(w, x.w, acc[3]);
-    }
-    const bool some = !(l == 0.0f);
-    const float inv = some ? 1.0f / l : 0.0f;
-    typedef T Four __attribute__((ext_vector_type(4)));
-    Four v;
+    const long long rows = (long long)off.Tq * Hq;
+    for (long long i = (long long)blockIdx.x * BLOCK + threadIdx.x; i < rows * packs; i += (long long)gridDim.x * BLOCK) {
+        const long long row = i / packs;
+        const int d = (int)(i % packs) * 4, head = (int)(row / off.Tq), t = (int)(row % off.Tq);
+        if (!clear && (t < clipped(off.q[0], off.Tq) || t >= clipped(off.q[off.B], off.Tq))) continue;  // (rows of no sequence stay)
+        float m = -INFINITY;
+        for (int s = 0; s < splits; ++s) m = fmaxf(m, part_lse[(size_t)s * rows + row]);
+        const float base = m == -INFINITY ? 0.0f : m;
+        float l = 0.0f, acc[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < splits; ++s) {
+            const float w = __builtin_amdgcn_exp2f(part_lse[(size_t)s * rows + row] - base);
+            const float4 x = *reinterpret_cast<const float4*>(part_out + ((size_t)s * rows + row) * D + d);
+            l += w;
+            acc[0] = fmaf(w, x.x, acc[0]);
+            acc[1] = fmaf(w, x.y, acc[1]);
+            acc[2] = fmaf(w, x.z, acc[2]);
+            acc[3] = fmaf(w, x.w, acc[3]);
+        }
+        const bool some = !(l == 0.0f);
+        const float inv = some ? 1.0f / l : 0.0f;
+        typedef T Four __attribute__((ext_vector_type(4)));
+        Four v;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = (T)(acc[k] * inv);
-    *reinterpret_cast<Four*>(out.p + (size_t)t * out.row + (size_t)head * out.head + d) = v;
-    if (d == 0 && lse) lse[row] = some ? (m + log2f(l)) * LN2 : -INFINITY;
+        for (int k = 0; k < 4; ++k) v[k] = (T)(acc[k] * inv);
+        *reinterpret_cast<Four*>(out.p + (size_t)t * out.row + (size_t)head * out.head + d) = v;
+        if (d == 0 && lse) lse[row] = some ? (m + log2f(l)) * LN2 : -INFINITY;
+    }
 }
 
 // ---- backward ---------------------------------------------------------------------------------------
@@ -537,24 +538,24 @@ __global__ __launch_bounds__(BLOCK) void join_kernel(const float* __restrict__ p
 template <typename T>
 __global__ __launch_bounds__(BLOCK) void delta_kernel(Heads<const T> gout, Heads<const T> out, int Tq, int Hq, int D,
                                                       float* __restrict__ delta) {
-    const long long row = ((long long)blockIdx.x * BLOCK + threadIdx.x) >> 4;  // token * Hq + head
-    if (row >= (long long)Tq * Hq) return;
-    const int t = (int)(row / Hq), head = (int)(row % Hq), d = ((int)threadIdx.x & 15) * 8;
-    float s = 0.0f;
-    if (d < D) {
-        const T* a = gout.p + (size_t)t * gout.row + (size_t)head * gout.head + d;
-        const T* b = out.p + (size_t)t * out.row + (size_t)head * out.head + d;
+    for (long long row = ((long long)blockIdx.x * BLOCK + threadIdx.x) >> 4; row < (long long)Tq * Hq; row += (long long)gridDim.x * BLOCK >> 4) {
+        const int t = (int)(row / Hq), head = (int)(row % Hq), d = ((int)threadIdx.x & 15) * 8;  // (row: t * Hq + head)
+        float s = 0.0f;
+        if (d < D) {
+            const T* a = gout.p + (size_t)t * gout.row + (size_t)head * gout.head + d;
+            const T* b = out.p + (size_t)t * out.row + (size_t)head * out.head + d;
 #pragma unroll
-        for (int c = 0; c < 8; c += 16 / (int)sizeof(T)) {
-            float x[16 / sizeof(T)], y[16 / sizeof(T)];
-            feat::load_pack(a + c, 8, x);
-            feat::load_pack(b + c, 8, y);
+            for (int c = 0; c < 8; c += 16 / (int)sizeof(T)) {
+                float x[16 / sizeof(T)], y[16 / sizeof(T)];
+                feat::load_pack(a + c, 8, x);
+                feat::load_pack(b + c, 8, y);
 #pragma unroll
-            for (int j = 0; j < 16 / (int)sizeof(T); ++j) s = fmaf(x[j], y[j], s);
+                for (int j = 0; j < 16 / (int)sizeof(T); ++j) s = fmaf(x[j], y[j], s);
+            }
         }
+        s = feat::over_lanes<Sum, 16>(s);
+        if ((threadIdx.x & 15) == 0) delta[(size_t)head * Tq + t] = s;
     }
-    s = feat::over_lanes<Sum, 16>(s);
-    if ((threadIdx.x & 15) == 0) delta[(size_t)head * Tq + t] = s;
 }
 
 // Gradients of the keys and values: a workgroup takes 128 keys, 32 a wave, and walks the rows (queries and heads of the group).
@@ -824,23 +825,24 @@ template <typename T>
 __global__ __launch_bounds__(BLOCK) void sum_kernel(const float* __restrict__ part, int splits, const int* __restrict__ off, int B, int rows,
                                                     int H, int D, int clear, Heads<T> out) {
     const int packs = D / 4;
-    const long long i = (long long)blockIdx.x * BLOCK + threadIdx.x, n = (long long)rows * H * packs;
-    if (i >= n) return;
-    const int t = (int)(i / ((long long)H * packs)), u = (int)(i % ((long long)H * packs)), head = u / packs, d = u % packs * 4;
-    if (!clear && (t < clipped(off[0], rows) || t >= clipped(off[B], rows))) return;
-    float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
-    for (int s = 0; s < splits; ++s) {
-        const float4 x = *reinterpret_cast<const float4*>(part + ((size_t)s * n + i) * 4);
-        a[0] += x.x;
-        a[1] += x.y;
-        a[2] += x.z;
-        a[3] += x.w;
-    }
-    typedef T Four __attribute__((ext_vector_type(4)));
-    Four v;
+    const long long n = (long long)rows * H * packs;
+    for (long long i = (long long)blockIdx.x * BLOCK + threadIdx.x; i < n; i += (long long)gridDim.x * BLOCK) {
+        const int t = (int)(i / ((long long)H * packs)), u = (int)(i % ((long long)H * packs)), head = u / packs, d = u % packs * 4;
+        if (!clear && (t < clipped(off[0], rows) || t >= clipped(off[B], rows))) continue;
+        float a[4] = {0.0f, 0.0f, 0.0f, 0.0f};
+        for (int s = 0; s < splits; ++s) {
+            const float4 x = *reinterpret_cast<const float4*>(part + ((size_t)s * n + i) * 4);
+            a[0] += x.x;
+            a[1] += x.y;
+            a[2] += x.z;
+            a[3] += x.w;
+        }
+        typedef T Four __attribute__((ext_vector_type(4)));
+        Four v;
 #pragma unroll
-    for (int k = 0; k < 4; ++k) v[k] = (T)a[k];
-    *reinterpret_cast<Four*>(out.p + (size_t)t * out.row + (size_t)head * out.head + d) = v;
+        for (int k = 0; k < 4; ++k) v[k] = (T)a[k];
+        *reinterpret_cast<Four*>(out.p + (size_t)t * out.row + (size_t)head * out.head + d) = v;
+    }
 }
 
 }  // namespace attn

@@ -118,6 +118,12 @@ bool apart(std::initializer_list<Span> all) {
     return true;
 }
 
+// Workgroups along an axis of a launch: fewer than 2^32 work items.  (More are not refused by the launch: it runs what is left of their
+// number modulo 2^32.)
+constexpr long long MAX_GROUPS = ((1ll << 32) - 1) / feat::BLOCK;
+// ... of a kernel that walks `items` work items with the whole grid
+unsigned groups_for(long long items) { return (unsigned)std::min((items + feat::BLOCK - 1) / feat::BLOCK, MAX_GROUPS); }
+
 // CALL(T) for the features' type
 #define FOR_TYPE(type, CALL)                           \
     do {                                               \
@@ -221,7 +227,8 @@ struct Attention {  // sizes of a call
 };
 bool valid(const Attention& a) {
     return known_type(a.type) && a.B >= 1 && a.B <= (1 << 24) && a.Tq >= 0 && a.Tk >= 0 && a.Tk <= (1 << 30) && a.Hq >= 1 && a.Hkv >= 1 &&
-           a.Hq % a.Hkv == 0 && a.Hkv <= 65535 && a.D >= 8 && a.D <= 128 && a.D % 8 == 0 && a.rows() <= (1ll << 30);
+           a.Hq % a.Hkv == 0 && a.Hkv <= 65535 && a.D >= 8 && a.D <= 128 && a.D % 8 == 0 && a.rows() <= (1ll << 30) &&
+           attn::tile_numbers(a.Tq, a.G(), 128, a.B) <= MAX_GROUPS && attn::tile_numbers(a.Tk, 1, 128, a.B) <= MAX_GROUPS;
 }
 
 // Into how many parts an axis of `length` on average is split, where there are `groups` workgroups without: so that the chip has
@@ -238,7 +245,7 @@ ForwardPlan forward_plan(const Attention& a) {
     const long long groups128 = (a.rows() / 128 + a.B) * a.Hkv, keys = a.Tk / a.B;
     ForwardPlan p;
     // short sequences and single tokens: 32 rows a workgroup, and too few groups of 128 to fill the chip
-    p.row_waves = a.rows() <= 48ll * a.B || groups128 < 256 ? 1 : 4;
+    p.row_waves = (a.rows() <= 48ll * a.B || groups128 < 256) && attn::tile_numbers(a.Tq, a.G(), 32, a.B) <= MAX_GROUPS ? 1 : 4;
     const long long groups = p.row_waves == 4 ? groups128 : (a.rows() / 32 + a.B) * a.Hkv;
     p.splits = splits_for(groups, keys, 256);
     return p;
@@ -466,7 +473,7 @@ int picasso_attention_forward(picasso_ctx* c, void* stream, int type, const pica
 #define PICASSO_CALL(T)                                                                                                       \
     FOR_WIDTH(T, D, PICASSO_WIDTH);                                                                                           \
     if (p.splits > 1)                                                                                                         \
-    attn::join_kernel<T><<<(unsigned)(((long long)Tq * Hq * (D / 4) + feat::BLOCK - 1) / feat::BLOCK), feat::BLOCK, 0, s>>>(   \
+    attn::join_kernel<T><<<groups_for((long long)Tq * Hq * (D / 4)), feat::BLOCK, 0, s>>>(                                      \
         part_out, part_lse, p.splits, off, Hq, D, clear_outside, heads<T>(out), d_lse)
     FOR_TYPE(type, PICASSO_CALL);
 #undef PICASSO_CALL
@@ -513,12 +520,16 @@ int picasso_attention_backward(picasso_ctx* c, void* stream, int type, const pic
             heads<const T>(gout), heads<const T>(q), heads<const T>(k), heads<const T>(v), d_lse, delta, off, Hq, Hkv, group, D,      \
             causal, clear_outside, sc, heads<T>(gq), part)
 #define PICASSO_SUM(T, splits, part, offsets, rows, H, to)                                                                         \
-    attn::sum_kernel<T><<<(unsigned)(((long long)(rows) * (H) * (D / 4) + feat::BLOCK - 1) / feat::BLOCK), feat::BLOCK, 0, s>>>(     \
+    attn::sum_kernel<T><<<groups_for((long long)(rows) * (H) * (D / 4)), feat::BLOCK, 0, s>>>(                                        \
         part, splits, offsets, B, rows, H, D, clear_outside, heads<T>(to))
+#define PICASSO_CALL(T)                                                                    \
+    attn::delta_kernel<T><<<groups_for((long long)Tq * Hq * 16), feat::BLOCK, 0, s>>>(heads<const T>(gout), heads<const T>(out), Tq, Hq, D, delta)
+    if (Tq > 0) {
+        FOR_TYPE(type, PICASSO_CALL);
+        LAUNCHED(c);  // (what follows reads it)
+    }
+#undef PICASSO_CALL
 #define PICASSO_CALL(T)                                                                                              \
-    if (Tq > 0)                                                                                                      \
-        attn::delta_kernel<T><<<(unsigned)(((long long)Tq * Hq * 16 + feat::BLOCK - 1) / feat::BLOCK), feat::BLOCK, 0, s>>>( \
-            heads<const T>(gout), heads<const T>(out), Tq, Hq, D, delta);                                            \
     if (Tk > 0) {                                                                                                    \
         FOR_WIDTH(T, D, PICASSO_KEYS);                                                                               \
         if (p.key_splits > 1) {                                                                                      \

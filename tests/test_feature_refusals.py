@@ -269,3 +269,14 @@ def test_clipping_overlaps(lib, pk):
     to = (ctypes.c_void_p * 2)(0x50000000, 0x60000000)
     for change in (dict(norm=x), dict(norm=0x50000000 + 400), dict(ws=0x60000000)):
         assert clip(out=to, **change) == pk.PICASSO_ERR_INVALID_ARG, change
+
+
+def test_attention_sizes_that_no_launch_holds(lib, pk):
+    """Fewer than 2^24 workgroups of 128 rows or keys; a sequence takes one at least."""
+    ask = lambda B, Tq, Tk, Hq=1: lib.picasso_attention_workspace_bytes(1, B, Tq, Tk, Hq, 1, 8, 1)  # noqa: E731
+    most = (1 << 24) - 3                                             # sequences without rows
+    assert ask(most, 1, 1) > 0 and ask(most + 1, 1, 1) == 0
+    assert ask(most - 1, 128, 1) > 0 and ask(most, 128, 1) == 0 and ask(most, 1, 128) == 0 and ask(most, 32, 1, 4) == 0
+    assert ask((1 << 23) - 3, 1 << 30, 1 << 30) > 0 and ask((1 << 23) - 2, 1 << 30, 1) == 0 and ask((1 << 23) - 2, 1, 1 << 30) == 0
+    far = dict(q=heads(pk, 0x100000000, 128), k=heads(pk, 0x200000000), v=heads(pk, 0x300000000), out=heads(pk, 0x400000000, 128))
+    assert forward(lib, pk, **far, B=most + 1) == pk.PICASSO_ERR_INVALID_ARG

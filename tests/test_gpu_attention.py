@@ -393,3 +393,26 @@ def test_outputs_as_parts_of_the_inputs_array(ctx):
         with pytest.raises(pk.PicassoError):
             ctx.picasso_attention_backward(go, q, k, v, to, lse, o, grads=(cut(g, 0), cut(g, 1), cut(g, 1)))
         assert all(torch.equal(cut(a, i), cut(before, i)) for i in range(3))
+
+
+def test_more_rows_than_work_items_of_one_launch(ctx):
+    """2^28 + 160 rows of 8 features: sixteen work items a row would be more than 2^32.  All queries (and all gradients of the outputs) are one
+    broadcast row of each head, so every row's results are those of a small call."""
+    if torch.cuda.mem_get_info()[0] < 30 << 30:
+        pytest.skip("less than 30 GB free")
+    T, H, D = (1 << 24) + 10, 16, 8
+    g = torch.Generator().manual_seed(2)
+    q, k, v, go = (torch.randn(n, h, D, generator=g).bfloat16().cuda() for n, h in ((1, H), (3, 1), (3, 1), (1, H)))
+    wide = lambda t, n: t.expand(n, H, D)  # noqa: E731
+    ko = offsets([3])
+    out, lse = ctx.picasso_attention_forward(wide(q, T), k, v, offsets([T]), ko)
+    gq, gk, gv = ctx.picasso_attention_backward(wide(go, T), wide(q, T), k, v, out, lse, offsets([T]), ko)
+    few = 40
+    out0, lse0 = ctx.picasso_attention_forward(wide(q, few), k, v, offsets([few]), ko)
+    gq0, _, _ = ctx.picasso_attention_backward(wide(go, few), wide(q, few), k, v, out0, lse0, offsets([few]), ko)
+    assert (gq0 != 0).any()
+    for name, big, small in (("out", out, out0), ("gq", gq, gq0)):
+        for i, c in enumerate(big.split(1 << 20)):
+            assert torch.equal(c, small[:1].expand_as(c)), (name, i << 20, (c != small[:1]).any(2).nonzero()[:3].tolist())
+    assert all((c == lse0[:, :1]).all() for c in lse.split(1 << 20, dim=1))
+    assert torch.isfinite(gk.float()).all() and torch.isfinite(gv.float()).all()
