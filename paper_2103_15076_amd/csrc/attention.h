@@ -107,16 +107,20 @@ inline long long tile_numbers(long long T, int times, int size, int B) { return 
 __device__ __forceinline__ int clipped(int x, int T) { return x < 0 ? 0 : (x > T ? T : x); }
 template <int SIZE>
 __device__ __forceinline__ Tile find_tile(const int* __restrict__ off, int B, int T, int times, long long number) {
-    // how many segments' numbers start at or below this one: counted, 64 at a time (descending offsets give some segment)
+    // the last segment whose numbers start at or below this one (their starts ascend): of 64 candidates spread over those left, one a
+    // lane, until they are neighbours; up to 62 sequences in one step, 2^24 in four.  (Descending offsets give some segment.)
     const int lane = (int)threadIdx.x & 63;
-    int count = 0;
-    for (int base = 0; base < B + 2; base += 64) {
-        const int i = base + lane;
-        const bool in = i < B + 2;
-        const int start = i <= 0 ? 0 : clipped(off[in ? i - 1 : 0], T);
-        count += __popcll(__ballot(in && (long long)start * times / SIZE + i <= number));
+    int seg = 0;
+    for (int left = B + 2; left > 1;) {
+        const int apart = (left + 63) >> 6, ahead = lane * apart;
+        const bool in = ahead < left;
+        const int i = in ? seg + ahead : 0;
+        const int start = i == 0 ? 0 : clipped(off[i - 1], T);
+        const int count = __popcll(__ballot(in && (long long)start * times / SIZE + i <= number));
+        const int skip = count > 0 ? (count - 1) * apart : 0;
+        seg += skip;
+        left = left - skip < apart ? left - skip : apart;
     }
-    const int seg = count - 1;
     Tile t;
     t.start = seg == 0 ? 0 : clipped(off[seg - 1], T);
     int end = seg == B + 1 ? T : clipped(off[seg], T);

@@ -416,3 +416,25 @@ def test_more_rows_than_work_items_of_one_launch(ctx):
             assert torch.equal(c, small[:1].expand_as(c)), (name, i << 20, (c != small[:1]).any(2).nonzero()[:3].tolist())
     assert all((c == lse0[:, :1]).all() for c in lse.split(1 << 20, dim=1))
     assert torch.isfinite(gk.float()).all() and torch.isfinite(gv.float()).all()
+
+
+@pytest.mark.parametrize("count", [62, 63, 64, 4000, 70_001, 300_000])
+def test_very_many_sequences(ctx, count):
+    """Sequences of 0 to 2 queries over 0 to 3 keys each, as many as `count`, against the same by sequences side by side in 64 bits."""
+    g = torch.Generator().manual_seed(count)
+    lq, lk = torch.randint(0, 3, (count,), generator=g), torch.randint(0, 4, (count,), generator=g)
+    cum = lambda n: torch.cat([torch.zeros(1, dtype=torch.long), n.cumsum(0)])  # noqa: E731
+    cq, ck = cum(lq), cum(lk)
+    q, k, v = (torch.randn(n, 1, 8, generator=g) for n in (int(cq[-1]), int(ck[-1]), int(ck[-1])))
+    out, lse = ctx.picasso_attention_forward(q.cuda(), k.cuda(), v.cuda(), cq.int().cuda(), ck.int().cuda(), scale=0.5)
+    of = torch.repeat_interleave(torch.arange(count), lq)                     # a query's sequence
+    at = (ck[:-1][of][:, None] + torch.arange(3)).clamp(max=len(k) - 1)       # its keys' rows
+    seen = torch.arange(3)[None, :] < lk[of][:, None]
+    s = torch.where(seen, 0.5 * (q.double() * k[:, 0].double()[at]).sum(2), -math.inf)
+    l = torch.logsumexp(s, 1)
+    p = torch.where(seen, torch.exp(s - torch.where(l == -math.inf, 0.0, l)[:, None]), 0.0)
+    want = (p[:, :, None] * v[:, 0].double()[at]).sum(1)
+    # (scores up to 20 of 8 products: (8 + 4) u 20, exponentials 8 u 21; all of it twice, values up to 6)
+    assert ((out[:, 0].double().cpu() - want).abs() <= 1000 * U * 6).all()
+    got = lse[0].double().cpu()
+    assert ((got == l) | ((got - l).abs() <= 1000 * U)).all()
