@@ -140,7 +140,7 @@ struct NormShape {
     int lanes, packs;
 };
 NormShape norm_shape(int C, int per_pack) {
-    const int q = (C + per_pack - 1) / per_pack;
+    const int q = (int)((C + per_pack - 1ll) / per_pack);
     NormShape s{1, 1};
     while (s.lanes < 64 && s.lanes < q) s.lanes *= 2;
     if (q > 256) s.lanes = feat::BLOCK;
@@ -184,18 +184,30 @@ NormSplit norm_split(long long N, int C, int type) {
     return NormSplit{chunk, (int)std::max(1ll, (N + chunk - 1) / chunk)};
 }
 
+// CALL(first row, rows) for launches of at most MAX_GROUPS workgroups of `per` rows each.
+template <typename Call>
+void by_rows(long long N, long long per, Call call) {
+    for (long long at = 0; at < N; at += per * MAX_GROUPS) call(at, std::min(per * MAX_GROUPS, N - at));
+}
+
 template <typename T>
 void launch_norm_forward(hipStream_t s, const T* x, long long N, int C, const float* gamma, const float* beta, float eps, T* y,
                          float* mean, float* rstd) {
+    const auto from = [](float* p, long long at) { return p ? p + at : nullptr; };
     if (C > lnorm::MAX_C) {
-        lnorm::forward_wide_kernel<T><<<(unsigned)N, feat::BLOCK, 0, s>>>(x, C, gamma, beta, eps, y, mean, rstd);
+        by_rows(N, 1, [&](long long at, long long n) {
+            lnorm::forward_wide_kernel<T><<<(unsigned)n, feat::BLOCK, 0, s>>>(x + at * C, C, gamma, beta, eps, y + at * C, from(mean, at), from(rstd, at));
+        });
         return;
     }
     const NormShape shape = norm_shape(C, feat::Chunk<T>::N);
-#define PICASSO_CALL(T, L, P)                                                                                  \
-    do {                                                                                                       \
-        const long long per = (long long)lnorm::rows_in_flight<L, P>() * lnorm::rows_per_block<L>();             \
-        lnorm::forward_kernel<T, L, P><<<(unsigned)((N + per - 1) / per), feat::BLOCK, 0, s>>>(x, N, C, gamma, beta, eps, y, mean, rstd); \
+#define PICASSO_CALL(T, L, P)                                                                                                   \
+    do {                                                                                                                        \
+        constexpr long long per = (long long)lnorm::rows_in_flight<L, P>() * lnorm::rows_per_block<L>();                         \
+        by_rows(N, per, [&](long long at, long long n) {                                                                        \
+            lnorm::forward_kernel<T, L, P><<<(unsigned)((n + per - 1) / per), feat::BLOCK, 0, s>>>(                              \
+                x + at * C, n, C, gamma, beta, eps, y + at * C, from(mean, at), from(rstd, at));                                \
+        });                                                                                                                     \
     } while (0)
     NORM_SHAPES(T, shape, PICASSO_CALL);
 #undef PICASSO_CALL
@@ -205,10 +217,12 @@ template <typename T>
 void launch_norm_backward(hipStream_t s, const T* gy, const T* x, long long N, int C, const float* gamma, const float* mean,
                           const float* rstd, T* gx, float* partial, const NormSplit& sp) {
     if (C > lnorm::MAX_C) {
-        if (gx && N) lnorm::backward_wide_kernel<T><<<(unsigned)N, feat::BLOCK, 0, s>>>(gy, x, C, gamma, mean, rstd, gx);
+        if (gx)
+            by_rows(N, 1, [&](long long at, long long n) {
+                lnorm::backward_wide_kernel<T><<<(unsigned)n, feat::BLOCK, 0, s>>>(gy + at * C, x + at * C, C, gamma, mean + at, rstd + at, gx + at * C);
+            });
         if (partial)
-            lnorm::columns_wide_kernel<T><<<dim3(sp.groups, (C + feat::BLOCK - 1) / feat::BLOCK), feat::BLOCK, 0, s>>>(
-                gy, x, N, C, mean, rstd, sp.chunk, partial);
+            lnorm::columns_wide_kernel<T><<<dim3(groups_for(C), sp.groups), feat::BLOCK, 0, s>>>(gy, x, N, C, mean, rstd, sp.chunk, partial);
         return;
     }
     const NormShape shape = norm_shape(C, feat::Chunk<T>::N);
@@ -426,8 +440,7 @@ int picasso_layer_norm_backward(picasso_ctx* c, void* stream, int type, const vo
     FOR_TYPE(type, PICASSO_CALL);
 #undef PICASSO_CALL
     if (sums)
-        lnorm::finish_kernel<<<(unsigned)((2ll * C + lnorm::FINISH_COLS - 1) / lnorm::FINISH_COLS), feat::BLOCK, 0, s>>>(partial, sp.groups, C, d_ggamma,
-                                                                                                             d_gbeta);
+        lnorm::finish_kernel<<<groups_for(2ll * C * (feat::BLOCK / lnorm::FINISH_COLS)), feat::BLOCK, 0, s>>>(partial, sp.groups, C, d_ggamma, d_gbeta);
     LAUNCHED(c);
     return PICASSO_OK;
 }

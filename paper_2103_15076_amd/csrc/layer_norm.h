@@ -130,15 +130,15 @@ __global__ __launch_bounds__(BLOCK) void forward_wide_kernel(const T* __restrict
     const long long n = blockIdx.x;
     const T* p = x + n * C;
     float s = 0.0f;
-    for (int c = threadIdx.x; c < C; c += BLOCK) s += (float)p[c];
+    for (unsigned c = threadIdx.x; c < (unsigned)C; c += BLOCK) s += (float)p[c];
     const float mean = row_sum(s) / (float)C;
     float q = 0.0f;
-    for (int c = threadIdx.x; c < C; c += BLOCK) {
+    for (unsigned c = threadIdx.x; c < (unsigned)C; c += BLOCK) {
         const float d = (float)p[c] - mean;
         q = fmaf(d, d, q);
     }
     const float rstd = 1.0f / sqrtf(row_sum(q) / (float)C + eps);
-    for (int c = threadIdx.x; c < C; c += BLOCK)
+    for (unsigned c = threadIdx.x; c < (unsigned)C; c += BLOCK)
         y[n * C + c] = (T)fmaf(((float)p[c] - mean) * rstd, gamma ? gamma[c] : 1.0f, beta ? beta[c] : 0.0f);
     if (threadIdx.x == 0) {
         if (mean_out) mean_out[n] = mean;
@@ -258,14 +258,14 @@ __global__ __launch_bounds__(BLOCK) void backward_wide_kernel(const T* __restric
     const size_t at = (size_t)blockIdx.x * C;
     const float mean = mean_in[blockIdx.x], rstd = rstd_in[blockIdx.x];
     float s1 = 0.0f, s2 = 0.0f;
-    for (int c = threadIdx.x; c < C; c += BLOCK) {
+    for (unsigned c = threadIdx.x; c < (unsigned)C; c += BLOCK) {
         const float h = (float)gy[at + c] * (gamma ? gamma[c] : 1.0f);
         s1 += h;
         s2 = fmaf(h, ((float)x[at + c] - mean) * rstd, s2);
     }
     s1 = row_sum(s1) / (float)C;
     s2 = row_sum(s2) / (float)C;
-    for (int c = threadIdx.x; c < C; c += BLOCK) {
+    for (unsigned c = threadIdx.x; c < (unsigned)C; c += BLOCK) {
         const float h = (float)gy[at + c] * (gamma ? gamma[c] : 1.0f);
         gx[at + c] = (T)(rstd * (h - s1 - ((float)x[at + c] - mean) * rstd * s2));
     }
@@ -274,17 +274,17 @@ template <typename T>
 __global__ __launch_bounds__(BLOCK) void columns_wide_kernel(const T* __restrict__ gy, const T* __restrict__ x, long long N, int C,
                                                              const float* __restrict__ mean_in, const float* __restrict__ rstd_in,
                                                              long long chunk, float* __restrict__ partial) {
-    const int c = blockIdx.y * BLOCK + threadIdx.x;
-    if (c >= C) return;
-    const long long first = (long long)blockIdx.x * chunk, last = first + chunk < N ? first + chunk : N;
+    const unsigned c = blockIdx.x * BLOCK + threadIdx.x;
+    if (c >= (unsigned)C) return;
+    const long long first = (long long)blockIdx.y * chunk, last = first + chunk < N ? first + chunk : N;
     float sg = 0.0f, sb = 0.0f;
     for (long long n = first; n < last; ++n) {
         const float g = (float)gy[n * C + c];
         sg = fmaf(g, ((float)x[n * C + c] - mean_in[n]) * rstd_in[n], sg);
         sb += g;
     }
-    partial[((size_t)blockIdx.x * 2 + 0) * C + c] = sg;
-    partial[((size_t)blockIdx.x * 2 + 1) * C + c] = sb;
+    partial[((size_t)blockIdx.y * 2 + 0) * C + c] = sg;
+    partial[((size_t)blockIdx.y * 2 + 1) * C + c] = sb;
 }
 
 // Columns of the workgroups' partials [groups][2 C] added up: 16 columns a workgroup, 16 lanes a column, each every 16th group in
@@ -292,27 +292,33 @@ __global__ __launch_bounds__(BLOCK) void columns_wide_kernel(const T* __restrict
 constexpr int FINISH_COLS = 16;
 __global__ __launch_bounds__(BLOCK) void finish_kernel(const float* __restrict__ partial, int groups, int C,
                                                        float* __restrict__ ggamma, float* __restrict__ gbeta) {
-    __shared__ double sums[BLOCK / FINISH_COLS][FINISH_COLS];
-    const int col = blockIdx.x * FINISH_COLS + (int)threadIdx.x % FINISH_COLS, part = (int)threadIdx.x / FINISH_COLS;
     constexpr int PARTS = BLOCK / FINISH_COLS;
-    double s = 0.0;
-    if (col < 2 * C) {
-        int g = part;
-        for (; g + 7 * PARTS < groups; g += 8 * PARTS) {
-            float v[8];
+    __shared__ double sums[PARTS][FINISH_COLS];
+    const int mine = (int)threadIdx.x % FINISH_COLS, part = (int)threadIdx.x / FINISH_COLS;
+    const long long cols = 2ll * C;
+    for (long long first = (long long)blockIdx.x * FINISH_COLS; first < cols; first += (long long)gridDim.x * FINISH_COLS) {
+        const long long col = first + mine;
+        double s = 0.0;
+        if (col < cols) {
+            int g = part;
+            for (; g + 7 * PARTS < groups; g += 8 * PARTS) {
+                float v[8];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) v[k] = partial[(size_t)(g + k * PARTS) * 2 * C + col];
+                for (int k = 0; k < 8; ++k) v[k] = partial[(g + k * PARTS) * cols + col];
 #pragma unroll
-            for (int k = 0; k < 8; ++k) s += (double)v[k];
+                for (int k = 0; k < 8; ++k) s += (double)v[k];
+            }
+            for (; g < groups; g += PARTS) s += (double)partial[g * cols + col];
         }
-        for (; g < groups; g += PARTS) s += (double)partial[(size_t)g * 2 * C + col];
+        sums[part][mine] = s;
+        __syncthreads();
+        if (part == 0 && col < cols) {
+            for (int k = 1; k < PARTS; ++k) s += sums[k][mine];
+            float* out = col < C ? ggamma : gbeta;
+            if (out) out[col < C ? col : col - C] = (float)s;
+        }
+        __syncthreads();
     }
-    sums[part][threadIdx.x % FINISH_COLS] = s;
-    __syncthreads();
-    if (part != 0 || col >= 2 * C) return;
-    for (int k = 1; k < PARTS; ++k) s += sums[k][threadIdx.x];
-    float* out = col < C ? ggamma : gbeta;
-    if (out) out[col < C ? col : col - C] = (float)s;
 }
 
 }  // namespace lnorm

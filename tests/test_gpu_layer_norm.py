@@ -175,3 +175,38 @@ def test_refusals(ctx):
         with pytest.raises(pk.PicassoError) as e:
             f()
         assert e.value.status == pk.PICASSO_ERR_INVALID_ARG
+
+
+def test_more_rows_than_workgroups_of_one_launch(ctx):
+    """2^24 + 3 rows that take a workgroup each (2056 channels of bfloat16): 256 work items a row would be more than 2^32."""
+    n, c, few = (1 << 24) + 3, 2056, 1 << 10
+    if torch.cuda.mem_get_info()[0] < 150 << 30:
+        pytest.skip("less than 150 GB free")
+    small = torch.randn(few, c, device="cuda").bfloat16()
+    want, m0, r0 = ctx.picasso_layer_norm_forward(small)
+    x = torch.empty(n, c, dtype=torch.bfloat16, device="cuda")
+    for part in x.split(few):
+        part.copy_(small[:len(part)])
+    y = torch.zeros_like(x)
+    _, mean, rstd = ctx.picasso_layer_norm_forward(x, out=y)
+    whole = n // few * few
+    for p in y[:whole].view(-1, few, c).split(64):
+        assert torch.equal(p, want.expand_as(p))
+    assert torch.equal(y[whole:], want[:n - whole])
+    assert torch.equal(mean[:whole].view(-1, few), m0.expand(whole // few, few)) and torch.equal(mean[whole:], m0[:n - whole])
+    assert torch.equal(rstd[:whole].view(-1, few), r0.expand(whole // few, few)) and torch.equal(rstd[whole:], r0[:n - whole])
+
+
+def test_more_columns_than_work_items_of_one_launch(ctx):
+    """2^27 + 5 channels: the columns' sums take 32 work items a channel, more than 2^32.  Features are +1 and -1, so that every sum over a
+    row is exact and xh is the feature within 2e-5 (eps 1e-5, and a mean below 1e-7)."""
+    c = (1 << 27) + 5
+    x = torch.ones(2, c, dtype=torch.bfloat16, device="cuda")
+    x[0, 1::2], x[1, 0::2] = -1, -1
+    gy = torch.randint(-8, 9, (2, c), device="cuda").bfloat16()
+    _, mean, rstd = ctx.picasso_layer_norm_forward(x)
+    assert (mean.abs() <= 1e-7).all() and ((rstd - 1).abs() <= 2e-5).all()
+    _, gg, gb = ctx.picasso_layer_norm_backward(gy, x, None, mean, rstd)
+    assert torch.equal(gb, gy[0].float() + gy[1].float())
+    want = gy[0].float() * x[0].float() + gy[1].float() * x[1].float()
+    assert ((gg - want).abs() <= 2e-5 * 16 + 1e-6).all()
