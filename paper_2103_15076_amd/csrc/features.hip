@@ -170,18 +170,24 @@ constexpr int NORM_MAX_PACKS = 8;
         }                                                                                                            \
     } while (0)
 
-// Workgroups of the backward pass, each with `chunk` rows and a partial sum of every column: as many as the chip holds at work
-// (four a compute unit), fewer where each would have less than a few turns of rows.
+// Workgroups of the backward pass, each with `chunk` rows and a partial sum of every column: 1024, fewer where each would have less
+// than a few turns of rows, more where a lane would add up more than RUN rows in binary32 (the partials are joined in 64 bits).
+// Partials are 8 bytes a channel for 64 rows or more that are read at 4 or 8 bytes and written at 2 or 4: 2 % of the traffic at most.
 struct NormSplit {
     long long chunk;
     int groups;
 };
+constexpr long long RUN = 64;
 NormSplit norm_split(long long N, int C, int type) {
-    const NormShape s = norm_shape(C, 16 / (int)size_of(type));
-    const long long turn = C > lnorm::MAX_C ? 64 : 2ll * std::max(1, feat::BLOCK / s.lanes);
-    long long groups = std::max(1ll, std::min(1024ll, (N + 2 * turn - 1) / (2 * turn)));
-    const long long chunk = std::max(1ll, ((N + groups - 1) / groups + turn - 1) / turn) * turn;
-    return NormSplit{chunk, (int)std::max(1ll, (N + chunk - 1) / chunk)};
+    const bool wide = C > lnorm::MAX_C;  // (a lane a column: all of a workgroup's rows are its own)
+    const long long beside = wide ? 1 : feat::BLOCK / norm_shape(C, 16 / (int)size_of(type)).lanes;
+    const long long turn = wide ? RUN : 2 * beside;
+    const long long groups = std::max(1ll, std::min(1024ll, (N + 2 * turn - 1) / (2 * turn)));
+    const long long chunk = std::min(RUN * beside, std::max(1ll, ((N + groups - 1) / groups + turn - 1) / turn) * turn);
+    // (columns_wide_kernel's workgroups along an axis that takes 65535)
+    const long long least = wide ? (N + 65534) / 65535 : (N + MAX_GROUPS - 1) / MAX_GROUPS;
+    const long long rows = std::max(chunk, (least + turn - 1) / turn * turn);
+    return NormSplit{rows, (int)std::max(1ll, (N + rows - 1) / rows)};
 }
 
 // CALL(first row, rows) for launches of at most MAX_GROUPS workgroups of `per` rows each.

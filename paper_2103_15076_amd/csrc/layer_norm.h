@@ -7,8 +7,8 @@
 // wave (or, for the widest that fit, a workgroup) share it, NP packs of 16 bytes a lane.  The mean is taken first and the
 // squares of the differences then, from the registers: nothing cancels, whatever the mean.  The backward pass makes all
 // gradients in one walk over gy and x: a lane sees the same columns of every row of its workgroup, so the columns' sums stay
-// in registers, and are joined in two fixed stages (lanes and waves; then workgroups' partials by finish_kernel): no atomics,
-// results do not depend on scheduling.
+// in registers, 64 rows a lane at most, and are joined in two fixed stages in 64 bits (a workgroup's rows side by side; then
+// workgroups' partials by finish_kernel): no atomics, results do not depend on scheduling.
 #pragma once
 #include "feature_types.h"
 
@@ -240,9 +240,9 @@ __global__ __launch_bounds__(BLOCK) void backward_kernel(const T* __restrict__ g
                     sums[((int)threadIdx.x / LANES) * COLS + (lane + i * LANES) * V + k] = which ? sb[i][k] : sg[i][k];
             __syncthreads();
             for (int c = threadIdx.x; c < C; c += BLOCK) {
-                float s = 0.0f;
-                for (int r = 0; r < R; ++r) s += sums[r * COLS + c];
-                out[(size_t)which * C + c] = s;
+                double s = 0.0;
+                for (int r = 0; r < R; ++r) s += (double)sums[r * COLS + c];
+                out[(size_t)which * C + c] = (float)s;
             }
         }
     }
@@ -288,7 +288,8 @@ __global__ __launch_bounds__(BLOCK) void columns_wide_kernel(const T* __restrict
 }
 
 // Columns of the workgroups' partials [groups][2 C] added up: 16 columns a workgroup, 16 lanes a column, each every 16th group in
-// turn, then a tree.  Sums are in 64 bits: there are up to some thousand groups of up to a few hundred rows each.
+// turn, then a tree.  Sums are in 64 bits, as those of a workgroup's rows side by side are; in binary32 a lane adds up 64 rows at most (of
+// rows wider than MAX_C a 65535th of all, where that is more).
 constexpr int FINISH_COLS = 16;
 __global__ __launch_bounds__(BLOCK) void finish_kernel(const float* __restrict__ partial, int groups, int C,
                                                        float* __restrict__ ggamma, float* __restrict__ gbeta) {

@@ -210,3 +210,18 @@ def test_more_columns_than_work_items_of_one_launch(ctx):
     assert torch.equal(gb, gy[0].float() + gy[1].float())
     want = gy[0].float() * x[0].float() + gy[1].float() * x[1].float()
     assert ((gg - want).abs() <= 2e-5 * 16 + 1e-6).all()
+
+
+@pytest.mark.parametrize("n,c,dtype", [(1 << 20, 1028, "f32"), (1 << 18, 8200, "f32"), (1 << 19, 2056, "bf16"), (1 << 23, 6, "f32")])
+def test_runs_of_the_columns_sums(ctx, n, c, dtype):
+    """However many rows there are, no more than 64 of them are added up in binary32 one behind the other, the rest in 64 bits: with a
+    gradient of one value everywhere (whose sums round the same way each time) the sum is off by 64 u for a run, u for each of the two values that
+    stand between the stages, and u for the result."""
+    value = 0.3321608006954193
+    x = torch.zeros(n, c, dtype=DTYPES[dtype], device="cuda")
+    gy = torch.full((n, c), value, dtype=DTYPES[dtype], device="cuda")
+    _, mean, rstd = ctx.picasso_layer_norm_forward(x)
+    _, gg, gb = ctx.picasso_layer_norm_backward(gy, x, None, mean, rstd)
+    want = float(gy[0, 0]) * n
+    assert ((gb.double() - want).abs() <= 67 * U * want).all(), float((gb.double() - want).abs().max()) / want / U
+    assert (gg == 0).all()
