@@ -575,7 +575,8 @@ size_t picasso_gradients_workspace_bytes(int32_t n, const int64_t* h_sizes) {
         if (h_sizes[k] < 0 || h_sizes[k] > (1ll << 44)) return 0;
     size_t partials = 0;
     gradient_tables(n, nullptr, nullptr, h_sizes, nullptr, [&](const grads::Table&, int groups) { partials += groups; });
-    return std::max<size_t>(partials, 1) * sizeof(double);
+    // (and their sum, where it is made first)
+    return std::max<size_t>(partials + (partials > grads::MAX_PARTIALS), 1) * sizeof(double);
 }
 
 int picasso_gradient_norm(picasso_ctx* c, void* stream, int32_t n, const void* const* h_grads, const int64_t* h_sizes,
@@ -605,7 +606,12 @@ int picasso_clip_gradients(picasso_ctx* c, void* stream, int32_t n, const void* 
     hipStream_t s = (hipStream_t)stream;
     ON_DEVICE(c);
     double* ws = (double*)d_workspace;
-    const int partials = queue_squares(s, n, h_grads, h_sizes, h_types, ws);
+    int partials = queue_squares(s, n, h_grads, h_sizes, h_types, ws);
+    if (partials > grads::MAX_PARTIALS) {
+        grads::total_kernel<<<1, feat::BLOCK, 0, s>>>(ws, partials, ws + partials);
+        ws += partials;
+        partials = 1;
+    }
     bool first = true;
     gradient_tables(n, h_grads, h_out, h_sizes, h_types, [&](const grads::Table& t, int groups) {
         grads::scale_kernel<<<groups, feat::BLOCK, 0, s>>>(t, ws, partials, max_norm, first ? d_norm : nullptr);

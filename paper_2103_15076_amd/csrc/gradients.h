@@ -3,10 +3,11 @@
 //   norm = sqrt(sum over tensors and values of g^2),  c = min(1, max_norm / (norm + 1e-6)),  out = c g
 //
 // Bound by memory: every value is read for the norm and, the coefficient being known only then, read again and written.
-// Two kernels: squares_kernel leaves a partial sum per workgroup, scale_kernel's workgroups each add all partials up (a few KB
-// from the caches, in one fixed order, so all arrive at the same norm), and scale.  Squares are summed in 64 bits: no
+// Two kernels: squares_kernel leaves a partial sum per workgroup, scale_kernel's workgroups each add all partials up (16 KB at
+// most from the caches, in one fixed order, so all arrive at the same norm), and scale.  Squares are summed in 64 bits: no
 // gradient's square leaves the range, and the sum's rounding does not depend on how many values there are.  The tensors'
-// table travels with the launch, TENSORS of them at a time.
+// table travels with the launch, TENSORS of them at a time; launches of many tables leave more partials than a workgroup should add
+// up for each 8192 values that it scales, and total_kernel makes one sum of them first.
 #pragma once
 #include "feature_types.h"
 
@@ -21,7 +22,7 @@ using feat::store_pack;
 
 constexpr int TENSORS = 120;              // per launch: the table stays below the 4 KB of a launch's arguments
 constexpr long long CHUNK_VALUES = 8192;  // values that a workgroup takes at a time
-constexpr int MAX_PARTIALS = 2048;        // per launch: eight workgroups a compute unit
+constexpr int MAX_PARTIALS = 2048;        // per launch: eight workgroups a compute unit; and those that scale_kernel adds up
 
 struct Table {
     const void* in[TENSORS];
@@ -100,8 +101,8 @@ __global__ __launch_bounds__(BLOCK) void squares_kernel(Table t, double* __restr
     if (threadIdx.x == 0) partial[blockIdx.x] = s;
 }
 
-// The norm from all partials, in every lane.
-__device__ __forceinline__ double norm_of(const double* __restrict__ partial, int partials, double* slots) {
+// The sum of all partials, in every lane.
+__device__ __forceinline__ double sum_of(const double* __restrict__ partial, int partials, double* slots) {
     double s = 0.0;
     int i = threadIdx.x;
     for (; i + 3 * BLOCK < partials; i += 4 * BLOCK) {
@@ -112,12 +113,18 @@ __device__ __forceinline__ double norm_of(const double* __restrict__ partial, in
         for (int k = 0; k < 4; ++k) s += v[k];
     }
     for (; i < partials; i += BLOCK) s += partial[i];
-    return sqrt(block_sum(s, slots));
+    return block_sum(s, slots);
+}
+
+__global__ __launch_bounds__(BLOCK) void total_kernel(const double* __restrict__ partial, int partials, double* __restrict__ total) {
+    __shared__ double slots[BLOCK / 64];
+    const double s = sum_of(partial, partials, slots);
+    if (threadIdx.x == 0) *total = s;
 }
 
 __global__ __launch_bounds__(BLOCK) void norm_kernel(const double* __restrict__ partial, int partials, float* __restrict__ norm) {
     __shared__ double slots[BLOCK / 64];
-    const double n = norm_of(partial, partials, slots);
+    const double n = sqrt(sum_of(partial, partials, slots));
     if (threadIdx.x == 0) *norm = (float)n;
 }
 
@@ -148,7 +155,7 @@ __device__ __forceinline__ void scale_chunk(const T* g, T* out, long long first,
 __global__ __launch_bounds__(BLOCK) void scale_kernel(Table t, const double* __restrict__ partial, int partials, double max_norm,
                                                       float* __restrict__ norm) {
     __shared__ double slots[BLOCK / 64];
-    const double n = norm_of(partial, partials, slots);
+    const double n = sqrt(sum_of(partial, partials, slots));
     if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)n;
     const double ratio = max_norm / (n + 1e-6);
     const float c = ratio >= 1.0 ? 1.0f : (float)ratio;

@@ -147,3 +147,11 @@ def test_tensors_that_only_a_generator_makes(ctx):
     for t, o in zip(g, out):
         w = min(1.0, 0.25 / (want + 1e-6)) * t.double()
         assert ((o.double() - w).abs() <= 2.002 * U * w.abs() + 2.0 ** -149).all()
+
+
+@pytest.mark.parametrize("count", [960, 2048, 2049, 6000])
+def test_very_many_tensors(ctx, count):
+    """As many partial sums as tensors, and more than one workgroup's share of them: they are added up once, not by every workgroup."""
+    check(ctx, tensors([(53 * k) % 300 + 1 for k in range(count)], [F32, F16], count), 1.5, False)
+    big = tensors([30_000 + k % 7 for k in range(count)], [BF16], count)   # (several workgroups a tensor)
+    check(ctx, big, 1.5, True)
