@@ -565,7 +565,7 @@ int picasso_attention_backward(picasso_ctx* ctx, void* stream, int type, const p
  * are read before the call returns.  h_out[k] may be h_grads[k]; no output overlaps another output or
  * another tensor (a tensor listed twice is refused).  max_norm >= 0, may be infinite.  A norm that is NaN
  * makes everything NaN, an infinite one makes finite gradients 0 and infinite ones NaN.
- * d_norm may be NULL in picasso_clip_gradients.  n >= 0, sizes >= 0. */
+ * d_norm may be NULL in picasso_clip_gradients.  n >= 0, sizes >= 0, 2^43 values together at most. */
 size_t picasso_gradients_workspace_bytes(int32_t n, const int64_t* h_sizes);
 int picasso_gradient_norm(picasso_ctx* ctx, void* stream, int32_t n, const void* const* h_grads, const int64_t* h_sizes,
                           const int32_t* h_types, float* d_norm, void* d_workspace, size_t workspace_bytes);

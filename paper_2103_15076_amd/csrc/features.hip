@@ -317,11 +317,9 @@ attn::Heads<T> heads(const picasso_heads* h) {
 
 // ---- gradients --------------------------------------------------------------------------------------
 
-struct GradientsPlan {
-    long long launches, partials;  // partials of all launches
-};
+// each(table, workgroups) for TENSORS tensors at a time (of sizes that `countable` has let pass).
 template <typename Each>
-bool gradient_tables(int n, const void* const* in, void* const* out, const int64_t* sizes, const int32_t* types, Each each) {
+void gradient_tables(int n, const void* const* in, void* const* out, const int64_t* sizes, const int32_t* types, Each each) {
     const int launches = std::max(1, (n + grads::TENSORS - 1) / grads::TENSORS);
     const int most = std::max(256, grads::MAX_PARTIALS / launches);
     for (int at = 0; at < n; at += grads::TENSORS) {
@@ -334,18 +332,26 @@ bool gradient_tables(int n, const void* const* in, void* const* out, const int64
             t.size_type[k] = (unsigned long long)sizes[at + k] << 2 | (unsigned)(types ? types[at + k] : 0);
             t.first[k] = (unsigned)chunks;
             chunks += ((unsigned long long)sizes[at + k] + grads::CHUNK_VALUES - 1) / grads::CHUNK_VALUES;
-            if (chunks > 0x7FFFFFFFull) return false;
         }
         t.first[t.count] = (unsigned)chunks;
         if (chunks) each(t, (int)std::min<unsigned long long>(chunks, most));
+    }
+}
+
+// Sizes whose chunks a table can number: 2^43 values in all (2^30 chunks of 8192, and one more a tensor).
+bool countable(int n, const int64_t* sizes) {
+    int64_t all = 0;
+    for (int k = 0; k < n; ++k) {
+        if (sizes[k] < 0 || sizes[k] > (1ll << 43) - all) return false;
+        all += sizes[k];
     }
     return true;
 }
 
 bool valid_gradients(int n, const void* const* in, const int64_t* sizes, const int32_t* types) {
-    if (n < 0 || (n > 0 && (!in || !sizes || !types))) return false;
+    if (n < 0 || (n > 0 && (!in || !sizes || !types)) || !countable(n, sizes)) return false;
     for (int k = 0; k < n; ++k)
-        if (sizes[k] < 0 || sizes[k] > (1ll << 44) || !known_type(types[k]) || (sizes[k] > 0 && !in[k]) || !aligned(in[k], size_of(types[k])))
+        if (!known_type(types[k]) || (sizes[k] > 0 && !in[k]) || !aligned(in[k], size_of(types[k])))
             return false;
     return true;
 }
@@ -570,9 +576,7 @@ int picasso_attention_backward(picasso_ctx* c, void* stream, int type, const pic
 }
 
 size_t picasso_gradients_workspace_bytes(int32_t n, const int64_t* h_sizes) {
-    if (n < 0 || (n > 0 && !h_sizes)) return 0;
-    for (int k = 0; k < n; ++k)
-        if (h_sizes[k] < 0 || h_sizes[k] > (1ll << 44)) return 0;
+    if (n < 0 || (n > 0 && !h_sizes) || !countable(n, h_sizes)) return 0;
     size_t partials = 0;
     gradient_tables(n, nullptr, nullptr, h_sizes, nullptr, [&](const grads::Table&, int groups) { partials += groups; });
     // (and their sum, where it is made first)

@@ -280,3 +280,14 @@ def test_attention_sizes_that_no_launch_holds(lib, pk):
     assert ask((1 << 23) - 3, 1 << 30, 1 << 30) > 0 and ask((1 << 23) - 2, 1 << 30, 1) == 0 and ask((1 << 23) - 2, 1, 1 << 30) == 0
     far = dict(q=heads(pk, 0x100000000, 128), k=heads(pk, 0x200000000), v=heads(pk, 0x300000000), out=heads(pk, 0x400000000, 128))
     assert forward(lib, pk, **far, B=most + 1) == pk.PICASSO_ERR_INVALID_ARG
+
+
+def test_more_values_than_can_be_numbered(lib, pk):
+    """Two tensors of 2^43 values were accepted, and nothing was done to them."""
+    two = (ctypes.c_int64 * 2)
+    for sizes in ((1 << 43, 1), (1 << 43, 1 << 43), (1 << 62, 1 << 62), (1, 1 << 44)):
+        assert lib.picasso_gradients_workspace_bytes(2, two(*sizes)) == 0
+        at, types = (ctypes.c_void_p * 2)(1 << 20, 1 << 60), (ctypes.c_int32 * 2)(0, 0)
+        assert lib.picasso_gradient_norm(CTX, None, 2, at, two(*sizes), types, P[0], P[9], BIG) == pk.PICASSO_ERR_INVALID_ARG
+        assert lib.picasso_clip_gradients(CTX, None, 2, at, two(*sizes), types, 1.0, at, None, P[9], BIG) == pk.PICASSO_ERR_INVALID_ARG
+    assert lib.picasso_gradients_workspace_bytes(2, two(1 << 42, 1 << 42)) >= 256 * 8
