@@ -22,8 +22,10 @@
 //
 // Rounding: scores, statistics and all sums are binary32.  For 16-bit features the probabilities and ds are rounded to the
 // features' type, as the matrix instructions take them: half a step each, relative, of terms of a sum whose result is rounded
-// to the same type.  binary16 has few exponents (a weight of one of a hundred thousand keys is below its normal range), so there
-// the probabilities are carried times 2^15 and ds times a power of two that keeps a key's or query's largest within the range (Range).
+// to the same type.  It costs: relative errors (root mean square) of 2.5e-3 for 1.7e-3 on causal bfloat16, 2.8e-4 for 2.1e-4 on
+// binary16, which operands of twice as many bits (a second product for the lower half of each) would spare.  delta is taken from out as stored.
+// binary16 has few exponents (a weight of one of a hundred thousand keys is below its normal range), so there the probabilities
+// are carried times 2^15 and ds times a power of two that keeps a key's or query's largest within the range (Range).
 #pragma once
 #include <type_traits>
 

@@ -2,7 +2,7 @@
 // features (binary32, bfloat16, binary16), packs of 16 bytes of them, and sums over lanes.
 //
 // Arithmetic is in binary32 whatever the features' type; a value is rounded to the features' type (to nearest even) once,
-// where it is stored.
+// where it is stored (and where it becomes an operand of a matrix instruction, attention.h).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
