@@ -542,8 +542,9 @@ typedef struct picasso_heads {
  * over the keys j of the sequence, numbered from its first; causal: over those with j <= i + (lk - lq), so that the
  * last query sees all.  A query that sees no key gets out = 0, lse = -inf.  out [Tq,Hq,D], d_lse [Hq,Tq] float32 (may be NULL).
  * Rows of no sequence (in front of the first, behind the last) are left as they were, or, with clear_outside, get what
- * a query without keys gets.  A causal call's non-finite keys and values may reach queries in front of them; those of
- * another sequence or of rows of none never do.  Hq a multiple of Hkv (at most 65535), D a multiple of 8 up to 128,
+ * a query without keys gets.  Non-finite values of another sequence, of rows of none or of queries that see no key reach nothing.
+ * Within a causal sequence those of keys and values may reach queries in front of them and, in the backward pass, those of
+ * queries and of gradients of outputs keys behind them.  Hq a multiple of Hkv (at most 65535), D a multiple of 8 up to 128,
  * Tq * Hq / Hkv and Tk up to 2^30, B and a 128th of either of them together up to 2^24 - 3, scale finite and positive. */
 size_t picasso_attention_workspace_bytes(int type, int32_t B, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv, int32_t D,
                                          int backward);

@@ -597,9 +597,9 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || DP <= 64 ? 2 : 1) void bac
     if (t.seq >= 0) sequence_rows(off.q, t.seq, off.Tq, &q_start, &lq);
     const int shift = t.len - lq;
     int r_begin = 0, r_end = lq * G;
-    if (causal) {  // rows that see the tile's first key, or a later one
+    if (causal) {  // rows that see the tile's first key, or a later one; the others (which may see nothing, and hold anything) are not read
         const long long first = ((long long)t.first - shift) * G;
-        r_begin = first <= 0 ? 0 : (first < r_end ? (int)first / S::ROWS * S::ROWS : r_end);
+        r_begin = first <= 0 ? 0 : (first < r_end ? (int)first : r_end);
     }
     if (splits > 1) {
         const int chunk = ((lq * G + splits - 1) / splits + S::ROWS - 1) / S::ROWS * S::ROWS;

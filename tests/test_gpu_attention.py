@@ -438,3 +438,39 @@ def test_very_many_sequences(ctx, count):
     assert ((out[:, 0].double().cpu() - want).abs() <= 1000 * U * 6).all()
     got = lse[0].double().cpu()
     assert ((got == l) | ((got - l).abs() <= 1000 * U)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("lq,lk,heads", [(50, 20, (2, 1)), (300, 177, (3, 1)), (40, 39, (1, 1)), (2500, 1100, (2, 2))])
+@pytest.mark.parametrize("bad", [math.nan, math.inf])
+def test_queries_that_see_no_key_reach_nothing(ctx, dtype, lq, lk, heads, bad):
+    """Causal, fewer keys than queries: whatever stands in the first rows of q and of the outputs' gradient, every result is the same."""
+    print(f"attention {dtype} lq={lq} lk={lk} {heads} {bad} in rows without keys", flush=True)
+    q, k, v, go = make([7, lq], [9, lk], *heads, 32, dtype, 4)
+    qo, ko = offsets([7, lq]), offsets([9, lk])
+    out, lse = ctx.picasso_attention_forward(q, k, v, qo, ko, causal=True)
+    want = ctx.picasso_attention_backward(go, q, k, v, out, lse, qo, ko, causal=True)
+    assert all(torch.isfinite(t.float()).all() for t in want)
+    rows = slice(7, 7 + lq - lk)
+    q[rows], go[rows] = bad, bad
+    o2, l2 = ctx.picasso_attention_forward(q, k, v, qo, ko, causal=True)
+    assert torch.equal(o2, out) and torch.equal(l2, lse)
+    for name, a, b in zip(("gq", "gk", "gv"), ctx.picasso_attention_backward(go, q, k, v, out, lse, qo, ko, causal=True), want):
+        assert torch.equal(a, b), name
+
+
+@pytest.mark.parametrize("dtype", ["f32", "f16"])
+@pytest.mark.parametrize("causal", [False, True])
+def test_non_finite_sequences_stay_by_themselves(ctx, dtype, causal):
+    lens = [70, 45, 33]
+    for which in range(4):
+        a = list(make(lens, lens, 2, 1, 40, dtype, 6))
+        o = offsets(lens)
+        first = lambda x: [t[s] for t in x for s in (slice(0, 70), slice(115, 148))]  # noqa: E731
+
+        def run(q, k, v, go):
+            out, lse = ctx.picasso_attention_forward(q, k, v, o, causal=causal)
+            return (out, lse.t()) + ctx.picasso_attention_backward(go, q, k, v, out, lse, o, causal=causal)
+        want = first(run(*a))
+        a[which][70:115] = math.nan if which % 2 else math.inf
+        assert all(torch.equal(x, y) for x, y in zip(first(run(*a)), want))
