@@ -423,9 +423,19 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || DP <= 64 ? 2 : 1) void for
         for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
             for (int r = 0; r < 16; ++r) most = fmaxf(most, s[kb][r]);
-        most = over_halves<Most>(most) * scale2;
-        const float now = fmaxf(m, most), base = now == -INFINITY ? 0.0f : now;
-        const float keep = __builtin_amdgcn_exp2f(m - base), raised = base - RAISE<T>;
+        most = over_halves<Most>(most);
+        const float now = fmaxf(m, most), base = now == -INFINITY ? 0.0f : now, base2 = base * scale2;
+        float keep = __builtin_amdgcn_exp2f(m * scale2 - base2), raised = base2 - RAISE<T>;
+        // (2^(s scale2 - base2) is off by the rounding of base2, which all of a row's weights share: it cancels.  Of scores so large that it
+        // could leave the exponents' range the difference is taken first.)
+        if (__ballot(fabsf(base2) > 0x1p20f)) {
+            keep = __builtin_amdgcn_exp2f((m - base) * scale2);
+            raised = -RAISE<T>;
+#pragma unroll
+            for (int kb = 0; kb < KB; ++kb)
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[kb][r] -= base;
+        }
         m = now;
         float sum = 0.0f;
 #pragma unroll
@@ -452,6 +462,7 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || DP <= 64 ? 2 : 1) void for
             }
     }
     l = over_halves<Sum>(l);
+    m *= scale2;
     if constexpr (S::KEY_WAVES > 1) {
         // the waves' statistics, then their sums, each wave's in turn
         static_assert(32 * DP * 4 <= S::LDS, "the sums of a wave fit the tiles' place");

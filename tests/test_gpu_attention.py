@@ -474,3 +474,31 @@ def test_non_finite_sequences_stay_by_themselves(ctx, dtype, causal):
         want = first(run(*a))
         a[which][70:115] = math.nan if which % 2 else math.inf
         assert all(torch.equal(x, y) for x, y in zip(first(run(*a)), want))
+
+
+@pytest.mark.parametrize("dtype,size", [("f32", 3e3), ("f32", 1e6), ("bf16", 1e6), ("f16", 8e3)])
+@pytest.mark.parametrize("lq,lk", [(100, 150), (40, 3000), (2, 9000)])
+@pytest.mark.parametrize("d", [64, 128])
+def test_scores_that_leave_binary32s_whole_numbers(ctx, dtype, size, lq, lk, d):
+    """Scores of 2^24 up to 2^41, which binary32 holds to some bits or thousands of bits: the weights still add up to 1 and are finite.  Where the
+    largest score is ahead by more than all roundings together (twice the bar of a score, and 40) the row is its key's value exactly."""
+    q, k, v, _ = make([lq], [lk], 2, 2, d, dtype, 3)
+    q, k = (q.float() * size).to(q.dtype), (k.float() * size).to(k.dtype)
+    out, lse = ctx.picasso_attention_forward(q, k, v, offsets([lq]), offsets([lk]))
+    scale = 1 / math.sqrt(d)
+    assert torch.isfinite(out.float()).all() and torch.isfinite(lse).all()
+    rows = 0
+    for x in range(2):
+        Q, K, V = (t[:, x].double() for t in (q, k, v))
+        s = scale * Q @ K.T
+        bar = (d + 4) * U * (scale * Q.abs() @ K.abs().T).amax(1) + 2 * U * s.abs().amax(1)
+        top = s.topk(2, dim=1)
+        sure = top.values[:, 0] - top.values[:, 1] > 2 * bar + 40
+        rows += int(sure.sum())
+        assert torch.equal(out[sure][:, x], v[top.indices[sure, 0], x])
+        assert ((lse[x].double() - top.values[:, 0]).abs() <= bar + 4 * U * top.values[:, 0].abs() + math.log(lk)).all()
+        # every output lies between the smallest and the largest value of its feature
+        h = torch.finfo(v.dtype).eps
+        assert (out[:, x].double() <= V.amax(0) + h * V.abs().amax(0) + (lk + 8) * U * 8).all()
+        assert (out[:, x].double() >= V.amin(0) - h * V.abs().amax(0) - (lk + 8) * U * 8).all()
+    assert rows > 0
