@@ -395,6 +395,13 @@ struct Where {
             number = PyObject_CallOneArg(g_current_stream, d);
             Py_DECREF(d);
         } else {
+            // (a kernel on a stream of another device than the current one, the context's, does not run where its tensors are)
+            PyObject* of = PyObject_GetAttrString(given, "device_index");
+            if (!of) throw PyError{};
+            const long index = PyLong_AsLong(of);
+            Py_DECREF(of);
+            if (index == -1 && PyErr_Occurred()) throw PyError{};
+            if (index != device) fail(PyExc_TypeError, "stream: expected a stream of the context's CUDA device");
             number = PyObject_GetAttrString(given, "cuda_stream");
         }
         if (!number) throw PyError{};

@@ -291,3 +291,18 @@ def test_more_values_than_can_be_numbered(lib, pk):
         assert lib.picasso_gradient_norm(CTX, None, 2, at, two(*sizes), types, P[0], P[9], BIG) == pk.PICASSO_ERR_INVALID_ARG
         assert lib.picasso_clip_gradients(CTX, None, 2, at, two(*sizes), types, 1.0, at, None, P[9], BIG) == pk.PICASSO_ERR_INVALID_ARG
     assert lib.picasso_gradients_workspace_bytes(2, two(1 << 42, 1 << 42)) >= 256 * 8
+
+
+@pytest.mark.parametrize("name", ["layer_norm_forward", "layer_norm_backward", "attention_forward", "attention_backward", "gradient_norm", "clip_gradients"])
+def test_streams_of_another_device(pk, name):
+    """Refused before any other argument is looked at (this one has no more)."""
+    pytest.importorskip("torch")
+    call = getattr(pk.binding._load_host(), name)
+
+    class Stream:
+        cuda_stream, device_index = 0, 1
+    with pytest.raises(TypeError, match="stream of the context's"):
+        call(CTX.value, 0, Stream())
+    Stream.device_index = 0
+    with pytest.raises(TypeError, match="too few"):
+        call(CTX.value, 0, Stream())
