@@ -502,3 +502,18 @@ def test_scores_that_leave_binary32s_whole_numbers(ctx, dtype, size, lq, lk, d):
         assert (out[:, x].double() <= V.amax(0) + h * V.abs().amax(0) + (lk + 8) * U * 8).all()
         assert (out[:, x].double() >= V.amin(0) - h * V.abs().amax(0) - (lk + 8) * U * 8).all()
     assert rows > 0
+
+
+# 128 rows a workgroup are taken from 256 of them on (rows / 128 and one a sequence, times the heads of keys), and the keys are split
+# where there are fewer than 512 and 512 keys or more a sequence.
+@pytest.mark.parametrize("dtype", ["f32", "bf16", "f16"])
+@pytest.mark.parametrize("d", [32, 64, 128])
+@pytest.mark.parametrize("causal", [False, True])
+@pytest.mark.parametrize("lq,lk,split", [([1500, 0, 1303, 1290], [300, 5, 417, 500], False), ([900, 1101], [900, 1101], True)])
+def test_128_rows_a_workgroup(ctx, dtype, d, causal, lq, lk, split):
+    import paper_2103_15076_amd as pk
+    groups = (sum(lq) * 2 // 128 + len(lq)) * 8
+    assert groups >= 512 if not split else 256 <= groups < 512
+    need = pk.load_library().picasso_attention_workspace_bytes({"f32": 0, "bf16": 1, "f16": 2}[dtype], len(lq), sum(lq), sum(lk), 16, 8, d, 0)
+    assert (need > 0) == split
+    check(ctx, lq, lk, 16, 8, d, dtype, causal, seed=d)
