@@ -465,8 +465,9 @@ class Context:
         return self._n.f2v_backward(self._p, stream, gx, y, pi, w, facets, offsets, bool(want_gpi))
 
     # ---- layer norm, attention, gradient clipping.  Tensors are float32, bfloat16 or float16 on the context's device; stream
-    # None: that device's current stream.  Outputs and workspaces come from torch's allocator, call by call; the calls wait for
-    # nothing and can be recorded into graphs.
+    # None: that device's current stream.  Outputs and workspaces come from torch's allocator, call by call (on a stream that is named,
+    # from that stream's memory); the calls wait for nothing and can be recorded into graphs.  What they write into a caller's tensors
+    # raises those tensors' versions.
 
     def picasso_layer_norm_forward(self, x, gamma=None, beta=None, eps=1e-5, out=None, stream=None):
         """Rows of x [N, C] normalised, times gamma plus beta (float32 [C]).  Returns (y[N,C], mean f32[N], rstd f32[N])."""

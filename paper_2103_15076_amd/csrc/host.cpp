@@ -4,6 +4,8 @@
 #include <Python.h>
 
 #include <ATen/ATen.h>
+#include <c10/core/StreamGuard.h>
+#include <c10/core/impl/VirtualGuardImpl.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -388,41 +390,50 @@ struct Where {
     PyObject* given;
     void* s;
     explicit Where(Args& a) : c(a.context()), device(a.i32()), given(a.next()) {
-        PyObject* number;
         if (given == Py_None) {
             PyObject* d = PyLong_FromLong(device);
             if (!d) throw PyError{};
-            number = PyObject_CallOneArg(g_current_stream, d);
+            PyObject* number = PyObject_CallOneArg(g_current_stream, d);
             Py_DECREF(d);
-        } else {
-            // (a kernel on a stream of another device than the current one, the context's, does not run where its tensors are)
-            PyObject* of = PyObject_GetAttrString(given, "device_index");
-            if (!of) throw PyError{};
-            const long index = PyLong_AsLong(of);
-            Py_DECREF(of);
-            if (index == -1 && PyErr_Occurred()) throw PyError{};
-            if (index != device) fail(PyExc_TypeError, "stream: expected a stream of the context's CUDA device");
-            number = PyObject_GetAttrString(given, "cuda_stream");
+            s = pointer(number);
+            return;
         }
-        if (!number) throw PyError{};
-        s = PyLong_AsVoidPtr(number);
-        Py_DECREF(number);
-        if (PyErr_Occurred()) throw PyError{};
+        // (a kernel on a stream of another device than the current one, the context's, does not run where its tensors are)
+        if (attribute("device_index") != device) fail(PyExc_TypeError, "stream: expected a stream of the context's CUDA device");
+        s = pointer(PyObject_GetAttrString(given, "cuda_stream"));
     }
-    at::TensorOptions on() const { return at::TensorOptions().device(at::Device(at::kCUDA, (at::DeviceIndex)device)); }
-    // A tensor that this call allocates.  Used on a stream that the caller names, the allocator learns of it.
-    at::Tensor empty(at::IntArrayRef shape, at::ScalarType type) const {
-        at::Tensor t = at::empty(shape, on().dtype(type));
-        if (given != Py_None) {
-            PyObject* w = THPVariable_Wrap(t);
-            PyObject* r = w ? PyObject_CallMethod(w, "record_stream", "O", given) : nullptr;
-            Py_XDECREF(r);
-            Py_XDECREF(w);
-            if (!r) throw PyError{};
-        }
+    // A tensor that this call allocates and returns.  On a stream that the caller names it comes from that stream's memory (what the
+    // current one has freed may still be in use there), and the allocator learns that the current one, the caller's, will use it.
+    at::Tensor empty(at::IntArrayRef shape, at::ScalarType type) const { return allocate(shape, type, true); }
+    // ... and one that only the call's kernels use.
+    at::Tensor workspace(size_t bytes) const { return allocate({(int64_t)std::max<size_t>(bytes, 16)}, at::kByte, false); }
+
+private:
+    at::Tensor allocate(at::IntArrayRef shape, at::ScalarType type, bool returned) const {
+        const c10::Device on(c10::DeviceType::CUDA, (c10::DeviceIndex)device);
+        const auto options = at::TensorOptions().device(on).dtype(type);
+        if (given == Py_None) return at::empty(shape, options);
+        const c10::Stream callers = c10::impl::VirtualGuardImpl(on.type()).getStream(on);
+        const c10::StreamGuard guard(c10::Stream::unpack3(attribute("stream_id"), on.index(), on.type()));
+        const at::Tensor t = at::empty(shape, options);
+        if (returned && callers != guard.current_stream() && t.numel()) t.record_stream(callers);
         return t;
     }
-    at::Tensor workspace(size_t bytes) const { return empty({(int64_t)std::max<size_t>(bytes, 16)}, at::kByte); }
+    static void* pointer(PyObject* number) {
+        if (!number) throw PyError{};
+        void* p = PyLong_AsVoidPtr(number);
+        Py_DECREF(number);
+        if (PyErr_Occurred()) throw PyError{};
+        return p;
+    }
+    long long attribute(const char* name) const {
+        PyObject* number = PyObject_GetAttrString(given, name);
+        if (!number) throw PyError{};
+        const long long v = PyLong_AsLongLong(number);
+        Py_DECREF(number);
+        if (v == -1 && PyErr_Occurred()) throw PyError{};
+        return v;
+    }
 };
 
 [[noreturn]] void wrong(const char* what, const char* expected) {

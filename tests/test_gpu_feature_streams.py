@@ -44,9 +44,8 @@ class Block:
         q, k, v = y.view(-1, hq + 2 * hkv, self.d).split([hq, hkv, hkv], dim=1)
         out, lse = ctx.picasso_attention_forward(q, k, v, self.o, causal=True, stream=stream)
         # (the gradients of q, k, v as parts of y's)
-        gy = torch.empty_like(y)
-        if stream is not None:
-            gy.record_stream(stream)   # (this one is the program's own)
+        with torch.cuda.stream(stream):    # (this one is the program's own)
+            gy = torch.empty_like(y)
         parts = gy.view(-1, hq + 2 * hkv, self.d).split([hq, hkv, hkv], dim=1)
         ctx.picasso_attention_backward(self.go, q, k, v, out, lse, self.o, causal=True, grads=parts, stream=stream)
         gx, gg, gb = ctx.picasso_layer_norm_backward(gy, self.x, self.gamma, mean, rstd, stream=stream)
@@ -106,6 +105,37 @@ def test_a_named_stream_is_told_to_the_allocator(ctx, block):
     side.synchronize()
     for k in kept:
         assert block.equal(k, want[-3:])
+
+
+def test_what_the_current_stream_still_writes_is_not_handed_out(ctx, block):
+    """Memory that the current stream has freed while its own kernels on it are still to come is none for a call on a named stream, which does
+    not wait for them; and a result that the current stream still reads when it is dropped is not handed out again before."""
+    want = block.run(ctx)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    a = torch.randn(4096, 4096, device="cuda")
+    torch.cuda.synchronize()
+    for _ in range(3):
+        b = a
+        for _ in range(20):
+            b = b @ a                                            # (some milliseconds in front of what follows on this stream)
+        junk = [torch.full_like(t, 9.0) for t in want]
+        del junk, b
+        got = block.run(ctx, stream=side)
+        side.synchronize()
+        torch.cuda.synchronize()
+        assert block.equal(got, want)
+        b = a
+        for _ in range(20):
+            b = b @ a
+        got[5].record_stream(torch.cuda.current_stream())        # (gy, the program's own)
+        copies = [t.clone() for t in got]                        # read by the current stream, late
+        del got, b
+        with torch.cuda.stream(side):
+            junk = [torch.full_like(t, 9.0) for t in want]
+        torch.cuda.synchronize()
+        assert block.equal(copies, want)
+        del junk, copies
 
 
 def test_recorded_into_a_graph(ctx, block):
