@@ -340,6 +340,7 @@ struct Scale {
     float plain;
 };
 
+// (Registers for two workgroups a compute unit: all fit but those of <16-bit, 128, 1>, where 5 go to memory.)
 template <typename T, int DP, int ROW_WAVES>
 __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || DP <= 64 ? 2 : 1) void forward_kernel(Heads<const T> q, Heads<const T> k, Heads<const T> v, Offsets off, int Hq,
                                                         int Hkv, Group group, int D, int causal, int clear, float scale2, Heads<T> out,
@@ -581,8 +582,9 @@ template <typename T, int DP>
 struct KeysShape {
     static constexpr int KEYS = 128, ROWS = 32;
     static constexpr int TILE = ROWS * DP;
-    // 16-bit rows of 128: a lane's key and value, two accumulators and two products are more than the 256 registers of two waves a
-    // SIMD; the values go to LDS
+    // 16-bit rows of 128: a lane's key and value, two accumulators and two products are far more than the 256 registers of two waves a
+    // SIMD; with the values in LDS 10 (bfloat16) to 15 (float16) registers still go to memory, some of them in every turn.  All that one LDS
+    // fragment feeds is one matrix instruction, and the kernel is bound by LDS: 1.92 of the 3.17 ms of causal 3 x 8 k, both passes.
     static constexpr bool VALUES_IN_LDS = sizeof(T) == 2 && DP == 128;
     static constexpr int BUFFERS = 4 * TILE * (int)sizeof(T) <= 80 * 1024 ? 2 : 1;
 };
@@ -644,7 +646,6 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || DP <= 64 ? 2 : 1) void bac
             const int row = r0 + r, i = group.query(row);
             *token = q_start + i;
             *head = kvh * G + row - i * G;
-            return row < r_end;
         };
         sq.load(D, r_end - r0, [&](int r) {
             int tk, hd;
@@ -658,7 +659,8 @@ __global__ __launch_bounds__(BLOCK, sizeof(T) == 2 || DP <= 64 ? 2 : 1) void bac
         });
         if ((int)threadIdx.x < 2 * S::ROWS) {
             int tk, hd;
-            const bool on = place((int)threadIdx.x % S::ROWS, &tk, &hd);
+            place((int)threadIdx.x % S::ROWS, &tk, &hd);
+            const bool on = r0 + (int)threadIdx.x % S::ROWS < r_end;
             const size_t at = (size_t)hd * off.Tq + tk;
             if ((int)threadIdx.x < S::ROWS) {
                 // rows of no keys, and those behind the last, have p = 0

@@ -147,7 +147,6 @@ NormShape norm_shape(int C, int per_pack) {
     while (s.lanes * s.packs < q) s.packs *= 2;
     return s;
 }
-constexpr int NORM_MAX_PACKS = 8;
 
 #define NORM_SHAPES(T, s, CALL)                                                                                      \
     do {                                                                                                             \
