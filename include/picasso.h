@@ -547,7 +547,7 @@ typedef struct picasso_heads {
  * queries and of gradients of outputs keys behind them.  Scores are binary32: forward, weights are right to a score's own rounding
  * however large it is; backward they are made from lse, off by 2^-23 of its magnitude: up to some thousands, not from 2^20 on.
  * Hq a multiple of Hkv (at most 65535), D a multiple of 8 up to 128,
- * Tq * Hq / Hkv and Tk up to 2^30, B and a 128th of either of them together up to 2^24 - 3, scale finite and positive. */
+ * Tq * Hq / Hkv and Tk up to 2^30, B and a 128th of either of them together up to 2^24 - 3, scale positive, up to 2^127. */
 size_t picasso_attention_workspace_bytes(int type, int32_t B, int32_t Tq, int32_t Tk, int32_t Hq, int32_t Hkv, int32_t D,
                                          int backward);
 int picasso_attention_forward(picasso_ctx* ctx, void* stream, int type, const picasso_heads* q, const picasso_heads* k,

@@ -250,6 +250,9 @@ bool valid(const Attention& a) {
            attn::tile_numbers(a.Tq, a.G(), 128, a.B) <= MAX_GROUPS && attn::tile_numbers(a.Tk, 1, 128, a.B) <= MAX_GROUPS;
 }
 
+// (the kernels take it times log2(e))
+bool valid_scale(float scale) { return scale > 0.0f && std::isfinite(scale * attn::LOG2E); }
+
 // Into how many parts an axis of `length` on average is split, where there are `groups` workgroups without: so that the chip has
 // two a compute unit, parts of at least `least`.
 int splits_for(long long groups, long long length, int least) {
@@ -468,7 +471,7 @@ int picasso_attention_forward(picasso_ctx* c, void* stream, int type, const pica
                               void* d_workspace, size_t workspace_bytes) {
     const Attention a{type, B, Tq, Tk, Hq, Hkv, D};
     if (!c || !valid(a) || !valid_heads(q, a, Tq, Hq, false) || !valid_heads(k, a, Tk, Hkv, false) || !valid_heads(v, a, Tk, Hkv, false) ||
-        !valid_heads(out, a, Tq, Hq, true) || !d_q_offsets || !d_k_offsets || !(scale > 0.0f) || !std::isfinite(scale))
+        !valid_heads(out, a, Tq, Hq, true) || !d_q_offsets || !d_k_offsets || !valid_scale(scale))
         return PICASSO_ERR_INVALID_ARG;
     const ForwardPlan p = forward_plan(a);
     const size_t need = attention_forward_bytes(a, p);
@@ -515,7 +518,7 @@ int picasso_attention_backward(picasso_ctx* c, void* stream, int type, const pic
     const Attention a{type, B, Tq, Tk, Hq, Hkv, D};
     if (!c || !valid(a) || !valid_heads(gout, a, Tq, Hq, false) || !valid_heads(q, a, Tq, Hq, false) || !valid_heads(k, a, Tk, Hkv, false) ||
         !valid_heads(v, a, Tk, Hkv, false) || !valid_heads(out, a, Tq, Hq, false) || !valid_heads(gq, a, Tq, Hq, true) ||
-        !valid_heads(gk, a, Tk, Hkv, true) || !valid_heads(gv, a, Tk, Hkv, true) || (Tq > 0 && !d_lse) || !d_q_offsets || !d_k_offsets || !(scale > 0.0f) || !std::isfinite(scale))
+        !valid_heads(gk, a, Tk, Hkv, true) || !valid_heads(gv, a, Tk, Hkv, true) || (Tq > 0 && !d_lse) || !d_q_offsets || !d_k_offsets || !valid_scale(scale))
         return PICASSO_ERR_INVALID_ARG;
     const BackwardPlan p = backward_plan(a);
     const size_t need = attention_backward_bytes(a, p), offsets = ((size_t)B + 1) * 4;

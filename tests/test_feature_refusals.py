@@ -306,3 +306,12 @@ def test_streams_of_another_device(pk, name):
     Stream.device_index = 0
     with pytest.raises(TypeError, match="too few"):
         call(CTX.value, 0, Stream())
+
+
+@pytest.mark.parametrize("scale", [2.5e38, 3.4e38])
+def test_scales_that_leave_the_range_in_units_of_a_bit(lib, pk, scale):
+    far = dict(q=heads(pk, 0x100000000, 128), k=heads(pk, 0x200000000), v=heads(pk, 0x300000000), out=heads(pk, 0x400000000, 128))
+    one = dict(far, Tq=1, Tk=100000, ws=None)      # (a call that lacks its workspace, so that none is accepted)
+    assert forward(lib, pk, **one, scale=scale) == pk.PICASSO_ERR_INVALID_ARG
+    assert forward(lib, pk, **one, scale=2.0 ** 127) == pk.PICASSO_ERR_WORKSPACE
+    assert forward(lib, pk, **one, scale=1e-45) == pk.PICASSO_ERR_WORKSPACE
