@@ -418,6 +418,26 @@ def test_more_rows_than_work_items_of_one_launch(ctx):
     assert torch.isfinite(gk.float()).all() and torch.isfinite(gv.float()).all()
 
 
+def test_more_heads_and_rows_than_32_bits_count(ctx):
+    """64 heads of keys, 2^25 + 7 queries: 2^31 rows and more in one launch, of which each axis counts for itself."""
+    if torch.cuda.mem_get_info()[0] < 120 << 30:
+        pytest.skip("less than 120 GB free")
+    T, H, D = (1 << 25) + 7, 64, 8
+    g = torch.Generator().manual_seed(3)
+    q, k, v, go = (torch.randn(n, H, D, generator=g).bfloat16().cuda() for n in (1, 2, 2, 1))
+    wide = lambda t, n: t.expand(n, H, D)  # noqa: E731
+    ko = offsets([2])
+    out, lse = ctx.picasso_attention_forward(wide(q, T), k, v, offsets([T]), ko)
+    gq, gk, gv = ctx.picasso_attention_backward(wide(go, T), wide(q, T), k, v, out, lse, offsets([T]), ko)
+    few = 40
+    out0, lse0 = ctx.picasso_attention_forward(wide(q, few), k, v, offsets([few]), ko)
+    gq0, _, _ = ctx.picasso_attention_backward(wide(go, few), wide(q, few), k, v, out0, lse0, offsets([few]), ko)
+    for name, big, small in (("out", out, out0), ("gq", gq, gq0)):
+        assert all(torch.equal(c, small[:1].expand_as(c)) for c in big.split(1 << 20)), name
+    assert all((c == lse0[:, :1]).all() for c in lse.split(1 << 20, dim=1))
+    assert torch.isfinite(gk.float()).all() and torch.isfinite(gv.float()).all()
+
+
 @pytest.mark.parametrize("count", [62, 63, 64, 4000, 70_001, 300_000])
 def test_very_many_sequences(ctx, count):
     """Sequences of 0 to 2 queries over 0 to 3 keys each, as many as `count`, against the same by sequences side by side in 64 bits."""
