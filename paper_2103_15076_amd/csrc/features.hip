@@ -255,7 +255,7 @@ bool valid_scale(float scale) { return scale > 0.0f && std::isfinite(scale * att
 
 // Into how many parts an axis of `length` on average is split, where there are `groups` workgroups without: so that the chip has
 // two a compute unit, parts of at least `least`.  Measured, backward pass alone, us with 1 / 2 / 4 / 8 splits of the rows: causal 3 x 8 k of 128
-// features (2 by the rule) 3629 / 2804 / 2183 / 2131; 16 x 1536 of 32, float32 (1) 751 / 705 / 681 / 698; causal 1 x 4 k of 64 (9)
+// features (2 by the rule) 3629 / 2804 / 2183 / 2131; 16 x 1536 of 32, float32 (1) 751 / 705 / 681 / 698; causal 1 x 4 k of 64 (8)
 // 663 / 392 / 250 / 173; 4 x 1000 of 64, float16 (4) 86 / 76 / 80 / 87.  Where lengths or, causal, the work of tiles differ more parts than
 // these would pay: the rule counts workgroups, not work.
 int splits_for(long long groups, long long length, int least) {
@@ -273,7 +273,7 @@ ForwardPlan forward_plan(const Attention& a) {
     // 128 to fill the chip.  Measured, us with 32 | 128 rows: one mesh of 500, 4 heads of 32, float32 11.7 | 26.9, of 4 k 114 | 125; of 2 k, 8 heads of 64,
     // float32 108 | 118; bfloat16, 8 heads over 2 of 64, 500 9.1 | 12.0, 1 k 21.0 | 16.8, 4 k 97.5 | 60.7; 8 heads of 128, 64 meshes of 40
     // 26.6 | 12.1, 256 of 16 38.3 | 25.7.  So 32 rows are right for one mesh of up to about a thousand and in float32, and lose by up to
-    // a factor of two among many short sequences and in 16 bits: the borders are cautious ones of the first kernels.
+    // a factor of two and more among many short sequences and in 16 bits.
     p.row_waves = (a.rows() <= 48ll * a.B || groups128 < 256) && attn::tile_numbers(a.Tq, a.G(), 32, a.B) <= MAX_GROUPS ? 1 : 4;
     const long long groups = p.row_waves == 4 ? groups128 : (a.rows() / 32 + a.B) * a.Hkv;
     p.splits = splits_for(groups, keys, 256);
