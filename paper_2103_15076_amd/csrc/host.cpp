@@ -634,32 +634,31 @@ PyObject* attention_backward(Args& a) {
 // queued, whatever becomes of the sequence: a generator's may have no other owner, and another thread may change a list.  (What
 // is allocated meanwhile must not get their memory.)
 struct Tensors {
-    std::vector<at::Tensor> held;
+    PyObject* held;  // a tuple: nothing changes it
     std::vector<const void*> data;
     std::vector<int64_t> sizes;
     std::vector<int32_t> types;
-    Tensors(PyObject* o, const Where& w, const char* what) {
-        PyObject* seq = PySequence_Fast(o, "expected a sequence of tensors");
-        if (!seq) throw PyError{};
+    Tensors(PyObject* o, const Where& w, const char* what) : held(PySequence_Tuple(o)) {
+        if (!held) throw PyError{};
         try {
-            const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
-            held.reserve(n), data.reserve(n), sizes.reserve(n), types.reserve(n);
+            const Py_ssize_t n = PyTuple_GET_SIZE(held);
+            data.reserve(n), sizes.reserve(n), types.reserve(n);
             for (Py_ssize_t k = 0; k < n; ++k) {
-                PyObject* item = PySequence_Fast_ITEMS(seq)[k];
-                if (!THPVariable_Check(item)) wrong(what, "a sequence of tensors");
-                const at::Tensor& t = THPVariable_Unpack(item);
+                if (!THPVariable_Check(PyTuple_GET_ITEM(held, k))) wrong(what, "a sequence of tensors");
+                const at::Tensor& t = (*this)[k];
                 if (!t.is_cuda() || t.get_device() != w.device || !t.is_contiguous()) wrong(what, "contiguous tensors on the context's CUDA device");
-                held.push_back(t);
                 types.push_back(type_of(t, what));
                 data.push_back(t.data_ptr());
                 sizes.push_back(t.numel());
             }
         } catch (...) {
-            Py_DECREF(seq);
+            Py_DECREF(held);
             throw;
         }
-        Py_DECREF(seq);
     }
+    ~Tensors() { Py_DECREF(held); }
+    Tensors(const Tensors&) = delete;
+    const at::Tensor& operator[](Py_ssize_t k) const { return THPVariable_Unpack(PyTuple_GET_ITEM(held, k)); }
     int n() const { return (int)data.size(); }
 };
 
@@ -691,7 +690,7 @@ PyObject* clip_gradients(Args& a) {
         return picasso_clip_gradients(w.c, w.s, g.n(), g.data.data(), g.sizes.data(), g.types.data(), max_norm, to.data(), F(norm), ws.data_ptr(),
                                       bytes);
     });
-    for (const at::Tensor& t : out ? out->held : g.held) written(t);
+    for (int k = 0; k < g.n(); ++k) written(out ? (*out)[k] : g[k]);
     return wrap(norm);
 }
 
