@@ -382,14 +382,21 @@ int tensors_apart(int n, const void* const* in, void* const* out, const int64_t*
     const auto add = [&](const void* p, uintptr_t bytes, bool written) {
         if (p && bytes) r.push_back(Range{(uintptr_t)p, (uintptr_t)p + bytes, written});
     };
+    // (outputs and gradients mostly ascend, each by themselves: sorted only where they do not)
+    const auto ascends = [](const Range& a, const Range& b) { return a.from < b.from; };
+    const auto sorted = [&](size_t first) {
+        if (!std::is_sorted(r.begin() + first, r.end(), ascends)) std::sort(r.begin() + first, r.end(), ascends);
+        std::inplace_merge(r.begin(), r.begin() + first, r.end(), ascends);
+        return r.size();
+    };
+    for (int k = 0; out && k < n; ++k) add(out[k], (uintptr_t)sizes[k] * size_of(types[k]), true);
+    const size_t outs = sorted(0);
+    for (int k = 0; k < n; ++k)
+        if (!out || out[k] != in[k]) add(in[k], (uintptr_t)sizes[k] * size_of(types[k]), false);
+    const size_t tensors = sorted(outs);
     add(norm, sizeof(float), true);
     add(ws, ws_bytes, true);
-    for (int k = 0; k < n; ++k) {
-        const uintptr_t bytes = (uintptr_t)sizes[k] * size_of(types[k]);
-        if (out) add(out[k], bytes, true);
-        if (!out || out[k] != in[k]) add(in[k], bytes, false);
-    }
-    std::sort(r.begin(), r.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+    sorted(tensors);
     uintptr_t end_out = 0, end_any = 0;  // of those that start before
     for (const Range& x : r) {
         if (x.from < (x.out ? end_any : end_out)) return PICASSO_ERR_INVALID_ARG;

@@ -315,3 +315,27 @@ def test_scales_that_leave_the_range_in_units_of_a_bit(lib, pk, scale):
     assert forward(lib, pk, **one, scale=scale) == pk.PICASSO_ERR_INVALID_ARG
     assert forward(lib, pk, **one, scale=2.0 ** 127) == pk.PICASSO_ERR_WORKSPACE
     assert forward(lib, pk, **one, scale=1e-45) == pk.PICASSO_ERR_WORKSPACE
+
+
+def test_clipping_overlaps_against_a_count_of_bytes(lib, pk):
+    """Tensors at random places in a short stretch of memory, some in place, in any order: refused exactly where a byte that is written is in
+    another tensor or in the norm."""
+    import random
+    rng = random.Random(11)
+    seen = {True: 0, False: 0}
+    for _ in range(6000):
+        n = rng.randint(1, 5)
+        base, room = 0x10000000, rng.choice((60, 400, 4000))
+        sizes, types = [rng.randint(0, 12) for _ in range(n)], [rng.randint(0, 2) for _ in range(n)]
+        at = [base + 4 * rng.randrange(room) for _ in range(n)]
+        to = [a if rng.random() < 0.5 else base + 4 * rng.randrange(room) for a in at]
+        norm = base + 4 * rng.randrange(room) if rng.random() < 0.5 else 0
+        cells = lambda p, k: set(range(p, p + sizes[k] * (4 if types[k] == 0 else 2)))  # noqa: E731
+        written, read = [cells(to[k], k) for k in range(n)] + [set(range(norm, norm + 4)) if norm else set()], [cells(at[k], k) if to[k] != at[k] else set() for k in range(n)]
+        over = sum(map(len, written)) > len(set().union(*written)) or bool(set().union(*written) & set().union(*read))
+        st = lib.picasso_clip_gradients(CTX, None, n, (ctypes.c_void_p * n)(*at), (ctypes.c_int64 * n)(*sizes), (ctypes.c_int32 * n)(*types), 1.0,
+                                        (ctypes.c_void_p * n)(*to), ctypes.c_void_p(norm), None, 0)
+        assert st in (pk.PICASSO_ERR_INVALID_ARG, pk.PICASSO_ERR_WORKSPACE)
+        assert (st == pk.PICASSO_ERR_INVALID_ARG) == over, (at, to, sizes, types, norm)
+        seen[over] += 1
+    assert min(seen.values()) > 1000
