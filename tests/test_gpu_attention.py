@@ -395,7 +395,15 @@ def test_outputs_as_parts_of_the_inputs_array(ctx):
         assert all(torch.equal(cut(a, i), cut(before, i)) for i in range(3))
 
 
-def test_more_rows_than_work_items_of_one_launch(ctx):
+@pytest.fixture
+def much_memory():
+    """What a test of many gigabytes took is given back, also to what does not allocate through torch."""
+    torch.cuda.empty_cache()
+    yield
+    torch.cuda.empty_cache()
+
+
+def test_more_rows_than_work_items_of_one_launch(ctx, much_memory):
     """2^28 + 160 rows of 8 features: sixteen work items a row would be more than 2^32.  All queries (and all gradients of the outputs) are one
     broadcast row of each head, so every row's results are those of a small call."""
     if torch.cuda.mem_get_info()[0] < 30 << 30:
@@ -418,7 +426,7 @@ def test_more_rows_than_work_items_of_one_launch(ctx):
     assert torch.isfinite(gk.float()).all() and torch.isfinite(gv.float()).all()
 
 
-def test_more_heads_and_rows_than_32_bits_count(ctx):
+def test_more_heads_and_rows_than_32_bits_count(ctx, much_memory):
     """64 heads of keys, 2^25 + 7 queries: 2^31 rows and more in one launch, of which each axis counts for itself."""
     if torch.cuda.mem_get_info()[0] < 120 << 30:
         pytest.skip("less than 120 GB free")

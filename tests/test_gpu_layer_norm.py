@@ -177,7 +177,15 @@ def test_refusals(ctx):
         assert e.value.status == pk.PICASSO_ERR_INVALID_ARG
 
 
-def test_more_rows_than_workgroups_of_one_launch(ctx):
+@pytest.fixture
+def much_memory():
+    """What a test of many gigabytes took is given back, also to what does not allocate through torch."""
+    torch.cuda.empty_cache()
+    yield
+    torch.cuda.empty_cache()
+
+
+def test_more_rows_than_workgroups_of_one_launch(ctx, much_memory):
     """2^24 + 3 rows that take a workgroup each (2056 channels of bfloat16): 256 work items a row would be more than 2^32."""
     n, c, few = (1 << 24) + 3, 2056, 1 << 10
     if torch.cuda.mem_get_info()[0] < 150 << 30:
@@ -197,7 +205,7 @@ def test_more_rows_than_workgroups_of_one_launch(ctx):
     assert torch.equal(rstd[:whole].view(-1, few), r0.expand(whole // few, few)) and torch.equal(rstd[whole:], r0[:n - whole])
 
 
-def test_more_columns_than_work_items_of_one_launch(ctx):
+def test_more_columns_than_work_items_of_one_launch(ctx, much_memory):
     """2^27 + 5 channels: the columns' sums take 32 work items a channel, more than 2^32.  Features are +1 and -1, so that every sum over a
     row is exact and xh is the feature within 2e-5 (eps 1e-5, and a mean below 1e-7)."""
     c = (1 << 27) + 5
@@ -213,7 +221,7 @@ def test_more_columns_than_work_items_of_one_launch(ctx):
 
 
 @pytest.mark.parametrize("n,c,dtype", [(1 << 20, 1028, "f32"), (1 << 18, 8200, "f32"), (1 << 19, 2056, "bf16"), (1 << 23, 6, "f32")])
-def test_runs_of_the_columns_sums(ctx, n, c, dtype):
+def test_runs_of_the_columns_sums(ctx, much_memory, n, c, dtype):
     """However many rows there are, no more than 64 of them are added up in binary32 one behind the other, the rest in 64 bits: with a
     gradient of one value everywhere (whose sums round the same way each time) the sum is off by 64 u for a run, u for each of the two values that
     stand between the stages, and u for the result."""
